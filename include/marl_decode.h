@@ -100,7 +100,8 @@ enum {
 enum {
   MARL_FLAG_BAD_GROUP = 1,       /* a group_of_seq entry was outside [0, NG) */
   MARL_FLAG_LEN_CLAMPED = 2,     /* a length was negative or exceeded its table row */
-  MARL_FLAG_BAD_PAGE = 4         /* a block-table entry of a valid token was outside [0, num_pages) */
+  MARL_FLAG_BAD_PAGE = 4,        /* a block-table entry of a valid token was outside [0, num_pages) */
+  MARL_FLAG_BAD_POSITION = 8     /* a position was outside the rotation's table (marl_qk_norm_rope) */
 };
 
 /* Fills *layout for *shape.  Host-only, no GPU needed.
@@ -361,6 +362,58 @@ int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, con
 int marl_grpo_advantages(const float* rewards, const int32_t* group_start,
                          const int32_t* group_seqs, int32_t num_groups, float eps, float* out,
                          void* stream);
+
+/*
+ * Norm of every query and key head and rotation by position, in one pass over the heads: what stands between the projections
+ * and the attention (or the cache) in the models that the paper trains.  For a head's row x of D = head_dim channels with its
+ * weight w (q_weight for query heads, k_weight for key heads):
+ *   r = 1 / sqrt(sum_d x_d^2 / D + eps),   y_d = x_d r w_d,
+ * and with rotary_dim = 2 h, cos and sin of the token's position t: c_i = cos_sin[t][i], s_i = cos_sin[t][h + i], for i < h
+ *   z_a = y_a c_i - y_b s_i,   z_b = y_b c_i + y_a s_i
+ * of the pair (a, b) = (i, i + h), or (2 i, 2 i + 1) with adjacent_pairs; z_d = y_d for d >= rotary_dim.
+ * Device arrays, `dtype` (bf16 or float32) unless said otherwise:
+ *   q, k             [num_tokens, num_q_heads, D] and [num_tokens, num_kv_heads, D]: a token's heads are contiguous, tokens lie
+ *                    q_stride / k_stride elements apart (slices of a fused projection's output; 0: the same row for all)
+ *   q_weight, k_weight [D], NULL: ones
+ *   cos_sin          float32 [max_positions, rotary_dim]; positions int32 [num_tokens] (both may be NULL if rotary_dim = 0)
+ *   q_out, k_out     the results, q_out_stride / k_out_stride apart; may be q and k themselves (with their strides)
+ * A position outside [0, max_positions) takes the nearest row of the table and sets MARL_FLAG_BAD_POSITION in *flags (device
+ * int32, may be NULL; OR-ed, the caller zeroes it).  Arithmetic in float32, one rounding when a result is stored.  A row with an
+ * infinity or a NaN gives unspecified values in that row alone.
+ *
+ * marl_qk_norm_rope_backward: from dq_out / dk_out, the gradients of q_out / k_out (strides q_out_stride / k_out_stride), and q, k:
+ *   dy = the rotation's transpose of dz;  g_d = dy_d w_d,  n_d = x_d r,
+ *   dx_d = r (g_d - n_d sum_e g_e n_e / D)              -> dq, dk [.., dq_stride / dk_stride apart]; may be dq_out and dk_out
+ *   dw_d = sum over tokens and heads of dy_d n_d        -> dq_weight, dk_weight float32 [D] (written, not added to; NULL: not wanted)
+ * The sums are formed in float32 in an order that the shape alone decides: the same bits in every run.  num_tokens = 0 writes zeros to
+ * dq_weight and dk_weight.  workspace: marl_qk_norm_rope_workspace_bytes() bytes, 16-byte aligned (needed by the backward call only).
+ * Every array but positions is accessed in 16-byte vectors: pointers must be 16-byte aligned, and strides multiples of 16 bytes
+ * (MARL_INVALID_ARG otherwise).
+ */
+typedef struct {
+  int32_t num_tokens;        /* >= 0 */
+  int32_t num_q_heads;       /* >= 1 */
+  int32_t num_kv_heads;      /* >= 1 */
+  int32_t head_dim;          /* 64, 128 or 256 */
+  int32_t rotary_dim;        /* a multiple of 16 in [0, head_dim] */
+  int32_t max_positions;     /* rows of cos_sin */
+  int32_t dtype;             /* MARL_OUT_BF16 or MARL_OUT_F32 */
+  int32_t adjacent_pairs;    /* 0: pairs (i, i + h); 1: pairs (2 i, 2 i + 1) */
+  float eps;                 /* finite, >= 0 */
+  int32_t reserved;          /* 0 */
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride;   /* elements between tokens; an output's at least its heads' width */
+  int64_t dq_stride, dk_stride;                             /* backward only */
+} marl_norm_rope_shape;
+
+int marl_qk_norm_rope(const marl_norm_rope_shape* shape, const void* q, const void* k, const void* q_weight,
+                      const void* k_weight, const float* cos_sin, const int32_t* positions, void* q_out,
+                      void* k_out, int32_t* flags, void* stream);
+int marl_qk_norm_rope_workspace_bytes(const marl_norm_rope_shape* shape, size_t* bytes);
+int marl_qk_norm_rope_backward(const marl_norm_rope_shape* shape, void* workspace, size_t workspace_bytes,
+                               const void* dq_out, const void* dk_out, const void* q, const void* k,
+                               const void* q_weight, const void* k_weight, const float* cos_sin,
+                               const int32_t* positions, void* dq, void* dk, float* dq_weight, float* dk_weight,
+                               int32_t* flags, void* stream);
 
 /*
  * Hierarchical load balancing of rollout requests (Section 5.2 of the paper), as a host-side,

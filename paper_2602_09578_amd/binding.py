@@ -24,7 +24,7 @@ MARL_OUT_BF16, MARL_OUT_F32 = 0, 1
 STAGES = ("plan", "prefix", "suffix", "merge", "logprob", "logprob_finish")
 CTR_NUM_SUFFIX_ITEMS, CTR_NUM_PREFIX_ITEMS, CTR_SUFFIX_CURSOR, CTR_PREFIX_CURSOR, CTR_FLAGS, \
     CTR_NUM_LONG_SUFFIX_ITEMS, CTR_SHORT_CURSOR, CTR_NUM_SHORT_PARTIAL_ITEMS = range(8)
-FLAG_BAD_GROUP, FLAG_LEN_CLAMPED, FLAG_BAD_PAGE = 1, 2, 4
+FLAG_BAD_GROUP, FLAG_LEN_CLAMPED, FLAG_BAD_PAGE, FLAG_BAD_POSITION = 1, 2, 4, 8
 
 
 class AttnShape(ctypes.Structure):
@@ -48,6 +48,12 @@ class PrefillShape(ctypes.Structure):
     _fields_ = [(n, I32) for n in (
         "num_tokens", "num_groups", "num_q_heads", "num_kv_heads", "head_dim", "page_size",
         "num_pages", "max_prefix_pages", "out_dtype", "reserved")]
+
+
+class NormRopeShape(ctypes.Structure):
+    _fields_ = [(n, I32) for n in ("num_tokens", "num_q_heads", "num_kv_heads", "head_dim", "rotary_dim", "max_positions",
+                                   "dtype", "adjacent_pairs")] + [("eps", ctypes.c_float), ("reserved", I32)] + \
+        [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride", "dq_stride", "dk_stride")]
 
 
 class BalancerConfig(ctypes.Structure):
@@ -165,6 +171,12 @@ def load_library(build_if_missing: bool = True):
     lib.marl_pack_tensors.argtypes = [VP, I32, ctypes.c_int64, VP, VP]
     lib.marl_unpack_tensors.argtypes = [VP, I32, ctypes.c_int64, VP, VP]
     lib.marl_pack_plan.restype = lib.marl_pack_tensors.restype = lib.marl_unpack_tensors.restype = ctypes.c_int
+    PN = ctypes.POINTER(NormRopeShape)
+    lib.marl_qk_norm_rope.argtypes = [PN] + [VP] * 10
+    lib.marl_qk_norm_rope_workspace_bytes.argtypes = [PN, ctypes.POINTER(SZ)]
+    lib.marl_qk_norm_rope_backward.argtypes = [PN, VP, SZ] + [VP] * 14
+    lib.marl_qk_norm_rope.restype = lib.marl_qk_norm_rope_workspace_bytes.restype = ctypes.c_int
+    lib.marl_qk_norm_rope_backward.restype = ctypes.c_int
     lib.marl_profile_begin.argtypes = [I32]
     lib.marl_profile_end.argtypes = [ctypes.POINTER(ctypes.c_float), ctypes.POINTER(I32), ctypes.POINTER(I32)]
     for f in ("marl_attn_plan_layout_for", "marl_workspace_bytes", "marl_decode_attn", "marl_decode_attn_static",
@@ -521,6 +533,78 @@ def prepare_prefill(inp, out_dtype=MARL_OUT_BF16):
 def run_prefill(inp, shape, ws, out):
     return marl_prefill_attn(shape, ws, inp.q, inp.k_pages, inp.v_pages, inp.prefix_block_table, inp.q_start,
                              inp.q_pos0, inp.scale, out)
+
+
+def _require_heads(t: torch.Tensor, name: str, dtype, tokens: int, heads, D) -> int:
+    """Rows [tokens, heads, D] whose heads are contiguous; their stride between tokens in elements."""
+    if not t.is_cuda:
+        raise ValueError("device tensors required: the library has no CPU path")
+    _require(t, name, dtype, (tokens, heads, D))
+    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+        raise ValueError(f"{name}: a token's heads have to be contiguous")
+    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1] * t.shape[2])
+
+
+def _norm_rope_shape(q, k, q_weight, k_weight, cos_sin, positions, eps, adjacent_pairs, flags) -> NormRopeShape:
+    if q.dim() != 3 or k.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("q, k: expected bf16 or float32 [tokens, heads, head_dim]")
+    T, Hq, D = q.shape
+    strides = _require_heads(q, "q", q.dtype, T, None, None), _require_heads(k, "k", q.dtype, T, None, D)
+    _require(q_weight, "q_weight", q.dtype, (D,))
+    _require(k_weight, "k_weight", q.dtype, (D,))
+    rot = 0
+    if cos_sin is not None:
+        _require(cos_sin, "cos_sin", torch.float32, (None, None))
+        rot = cos_sin.shape[1]
+        if rot > 0:
+            if positions is None:
+                raise ValueError("positions: needed for the rotation")
+            _require(positions, "positions", torch.int32, (T,))
+    _require(flags, "flags", torch.int32)
+    _require_cuda(q_weight, k_weight, cos_sin, positions if rot else None, flags)
+    return NormRopeShape(T, Hq, k.shape[1], D, rot, cos_sin.shape[0] if rot else 0, MARL_OUT_BF16 if q.dtype == torch.bfloat16 else MARL_OUT_F32,
+                         int(bool(adjacent_pairs)), float(eps), 0, *strides, 0, 0, 0, 0)
+
+
+def marl_qk_norm_rope(q, k, q_weight, k_weight, cos_sin, positions, eps: float, q_out, k_out, adjacent_pairs: bool = False,
+                      flags: Optional[torch.Tensor] = None):
+    """Norm of every head of q [tokens, Hq, D] and k [tokens, Hkv, D] with its weight, then rotation by position: see the header.
+    cos_sin: float32 [max_positions, rotary_dim], or None for none.  q_out and k_out may be q and k themselves."""
+    shape = _norm_rope_shape(q, k, q_weight, k_weight, cos_sin, positions, eps, adjacent_pairs, flags)
+    shape.q_out_stride = _require_heads(q_out, "q_out", q.dtype, *q.shape)
+    shape.k_out_stride = _require_heads(k_out, "k_out", q.dtype, *k.shape)
+    rc = load_library().marl_qk_norm_rope(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight),
+                                          _ptr(cos_sin) if shape.rotary_dim else None, _ptr(positions) if shape.rotary_dim else None,
+                                          _ptr(q_out), _ptr(k_out), _ptr(flags), _stream(q.device))
+    _check(rc, "marl_qk_norm_rope")
+    return q_out, k_out
+
+
+def marl_qk_norm_rope_workspace_bytes(num_tokens: int, num_q_heads: int, num_kv_heads: int, head_dim: int) -> int:
+    n = SZ(0)
+    shape = NormRopeShape(num_tokens, num_q_heads, num_kv_heads, head_dim, 0, 0, MARL_OUT_BF16, 0, 0.0, 0, 0, 0, 0, 0, 0, 0)
+    _check(load_library().marl_qk_norm_rope_workspace_bytes(ctypes.byref(shape), ctypes.byref(n)), "marl_qk_norm_rope_workspace_bytes")
+    return int(n.value)
+
+
+def marl_qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos_sin, positions, eps: float, dq, dk, dq_weight, dk_weight,
+                               workspace: torch.Tensor, adjacent_pairs: bool = False, flags: Optional[torch.Tensor] = None):
+    """Gradients dq, dk (which may be dq_out and dk_out themselves) and dq_weight, dk_weight (float32, None: not wanted) of
+    marl_qk_norm_rope from those of its results."""
+    shape = _norm_rope_shape(q, k, q_weight, k_weight, cos_sin, positions, eps, adjacent_pairs, flags)
+    shape.q_out_stride = _require_heads(dq_out, "dq_out", q.dtype, *q.shape)
+    shape.k_out_stride = _require_heads(dk_out, "dk_out", q.dtype, *k.shape)
+    shape.dq_stride = _require_heads(dq, "dq", q.dtype, *q.shape)
+    shape.dk_stride = _require_heads(dk, "dk", q.dtype, *k.shape)
+    _require(dq_weight, "dq_weight", torch.float32, (shape.head_dim,))
+    _require(dk_weight, "dk_weight", torch.float32, (shape.head_dim,))
+    _require_cuda(dq_weight, dk_weight, workspace)
+    rc = load_library().marl_qk_norm_rope_backward(
+        ctypes.byref(shape), _ptr(workspace), workspace.numel(), _ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight),
+        _ptr(cos_sin) if shape.rotary_dim else None, _ptr(positions) if shape.rotary_dim else None,
+        _ptr(dq), _ptr(dk), _ptr(dq_weight), _ptr(dk_weight), _ptr(flags), _stream(q.device))
+    _check(rc, "marl_qk_norm_rope_backward")
+    return dq, dk, dq_weight, dk_weight
 
 
 class Balancer:

@@ -769,6 +769,119 @@ int marl_grpo_advantages(const float* rewards, const int32_t* group_start, const
   return e == hipSuccess ? MARL_OK : hip_fail(e, "advantage kernel");
 }
 
+// ---- norm of query and key heads with the rotation ----------------------------------------------
+namespace {
+int check_norm_rope_shape(const marl_norm_rope_shape* s) {
+  if (!s) return MARL_INVALID_ARG;
+  if (s->num_tokens < 0 || s->num_q_heads < 1 || s->num_kv_heads < 1 || s->rotary_dim < 0 || s->rotary_dim > s->head_dim ||
+      s->max_positions < 0 || (s->rotary_dim > 0 && s->max_positions < 1) || !isfinite(s->eps) || s->eps < 0.f)
+    return MARL_INVALID_ARG;
+  if (s->head_dim != 64 && s->head_dim != 128 && s->head_dim != 256) return MARL_UNSUPPORTED;
+  if (s->rotary_dim % 16 != 0 || (s->dtype != MARL_OUT_BF16 && s->dtype != MARL_OUT_F32) || (s->adjacent_pairs != 0 && s->adjacent_pairs != 1))
+    return MARL_UNSUPPORTED;
+  if ((long)s->num_tokens * ((long)s->num_q_heads + s->num_kv_heads) >= (1L << 31)) return MARL_UNSUPPORTED;   // 32-bit row indices
+  return MARL_OK;
+}
+// An array of tokens: an address that the kernels can read (or, for an output, also write without overlap) as 16-byte vectors.
+bool norm_rope_rows_ok(const marl_norm_rope_shape* s, const void* p, int64_t stride, int32_t heads, bool output) {
+  const int64_t width = (int64_t)heads * s->head_dim, size = s->dtype == MARL_OUT_F32 ? 4 : 2;
+  return p && aligned16(p) && stride >= 0 && stride < ((int64_t)1 << 40) && stride * size % 16 == 0 && (!output || stride >= width || s->num_tokens == 1);
+}
+int fill_norm_rope_args(const marl_norm_rope_shape* s, const void* q, const void* k, const void* q_weight, const void* k_weight,
+                        const float* cos_sin, const int32_t* positions, int32_t* flags, marl::NormRopeArgs& a) {
+  if (!norm_rope_rows_ok(s, q, s->q_stride, s->num_q_heads, false) || !norm_rope_rows_ok(s, k, s->k_stride, s->num_kv_heads, false))
+    return MARL_INVALID_ARG;
+  if (s->rotary_dim > 0 && (!cos_sin || !positions || !aligned16(cos_sin))) return MARL_INVALID_ARG;
+  if (!aligned16(q_weight) || !aligned16(k_weight)) return MARL_INVALID_ARG;
+  a.q = q;
+  a.k = k;
+  a.q_weight = q_weight;
+  a.k_weight = k_weight;
+  a.cos_sin = cos_sin;
+  a.positions = positions;
+  a.flags = flags;
+  return MARL_OK;
+}
+void fill_norm_rope_shape(const marl_norm_rope_shape* s, marl::NormRopeArgs& a) {
+  memset(&a, 0, sizeof a);
+  a.T = s->num_tokens;
+  a.Hq = s->num_q_heads;
+  a.Hkv = s->num_kv_heads;
+  a.D = s->head_dim;
+  a.rotary_dim = s->rotary_dim;
+  a.max_positions = s->max_positions;
+  a.eps = s->eps;
+  a.f32 = s->dtype == MARL_OUT_F32;
+  a.adjacent = s->adjacent_pairs != 0;
+  a.q_stride = s->q_stride;
+  a.k_stride = s->k_stride;
+  a.q_out_stride = s->q_out_stride;
+  a.k_out_stride = s->k_out_stride;
+  a.dq_stride = s->dq_stride;
+  a.dk_stride = s->dk_stride;
+}
+}  // namespace
+
+int marl_qk_norm_rope(const marl_norm_rope_shape* shape, const void* q, const void* k, const void* q_weight,
+                      const void* k_weight, const float* cos_sin, const int32_t* positions, void* q_out,
+                      void* k_out, int32_t* flags, void* stream) {
+  int rc = check_norm_rope_shape(shape);
+  if (rc != MARL_OK) return rc;
+  if (shape->num_tokens == 0) return MARL_OK;
+  marl::NormRopeArgs a;
+  fill_norm_rope_shape(shape, a);
+  rc = fill_norm_rope_args(shape, q, k, q_weight, k_weight, cos_sin, positions, flags, a);
+  if (rc != MARL_OK) return rc;
+  if (!norm_rope_rows_ok(shape, q_out, shape->q_out_stride, shape->num_q_heads, true) ||
+      !norm_rope_rows_ok(shape, k_out, shape->k_out_stride, shape->num_kv_heads, true))
+    return MARL_INVALID_ARG;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  const hipError_t e = marl::launch_qk_norm_rope(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? MARL_OK : hip_fail(e, "norm and rotation kernel");
+}
+
+int marl_qk_norm_rope_workspace_bytes(const marl_norm_rope_shape* shape, size_t* bytes) {
+  const int rc = check_norm_rope_shape(shape);
+  if (rc != MARL_OK) return rc;
+  if (!bytes) return MARL_INVALID_ARG;
+  *bytes = (size_t)marl::kNormRopeMaxBlocks * 2 * shape->head_dim * sizeof(float);
+  return MARL_OK;
+}
+
+int marl_qk_norm_rope_backward(const marl_norm_rope_shape* shape, void* workspace, size_t workspace_bytes,
+                               const void* dq_out, const void* dk_out, const void* q, const void* k,
+                               const void* q_weight, const void* k_weight, const float* cos_sin,
+                               const int32_t* positions, void* dq, void* dk, float* dq_weight, float* dk_weight,
+                               int32_t* flags, void* stream) {
+  size_t need = 0;
+  int rc = marl_qk_norm_rope_workspace_bytes(shape, &need);
+  if (rc != MARL_OK) return rc;
+  marl::NormRopeArgs a;
+  fill_norm_rope_shape(shape, a);
+  if (reinterpret_cast<uintptr_t>(dq_weight) % 4 != 0 || reinterpret_cast<uintptr_t>(dk_weight) % 4 != 0) return MARL_INVALID_ARG;
+  a.dq_weight = dq_weight;
+  a.dk_weight = dk_weight;
+  if (shape->num_tokens > 0) {
+    rc = fill_norm_rope_args(shape, q, k, q_weight, k_weight, cos_sin, positions, flags, a);
+    if (rc != MARL_OK) return rc;
+    if (!norm_rope_rows_ok(shape, dq_out, shape->q_out_stride, shape->num_q_heads, false) ||
+        !norm_rope_rows_ok(shape, dk_out, shape->k_out_stride, shape->num_kv_heads, false) ||
+        !norm_rope_rows_ok(shape, dq, shape->dq_stride, shape->num_q_heads, true) ||
+        !norm_rope_rows_ok(shape, dk, shape->dk_stride, shape->num_kv_heads, true))
+      return MARL_INVALID_ARG;
+    if (!workspace || !aligned16(workspace)) return MARL_INVALID_ARG;
+    if (workspace_bytes < need) return MARL_WORKSPACE_TOO_SMALL;
+    a.dq_out = dq_out;
+    a.dk_out = dk_out;
+    a.dq = dq;
+    a.dk = dk;
+    a.partials = static_cast<float*>(workspace);
+  }
+  const hipError_t e = marl::launch_qk_norm_rope_backward(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? MARL_OK : hip_fail(e, "norm and rotation backward kernels");
+}
+
 // ---- weight synchronisation as one copy ------------------------------------------------------
 int marl_pack_plan(marl_pack_entry* entries, int32_t n, uint64_t* packed_bytes, int64_t* total_chunks) {
   if (n < 0 || !packed_bytes || !total_chunks || (n > 0 && !entries)) return MARL_INVALID_ARG;

@@ -180,4 +180,31 @@ struct GrpoArgs {
 };
 hipError_t launch_grpo_advantages(const GrpoArgs& a, hipStream_t st);
 
+struct NormRopeArgs {
+  const void* q;                // [T][Hq][D], tokens q_stride elements apart
+  const void* k;                // [T][Hkv][D]
+  const void* q_weight;         // [D] or null: ones
+  const void* k_weight;
+  const float* cos_sin;         // [max_positions][rotary_dim]: cosines, then sines
+  const int32_t* positions;     // [T]
+  void* q_out;                  // forward: results
+  void* k_out;
+  const void* dq_out;           // backward: gradients of the results, with the results' strides
+  const void* dk_out;
+  void* dq;
+  void* dk;
+  float* dq_weight;             // [D], may be null
+  float* dk_weight;
+  float* partials;              // backward: [workgroups][2 D]
+  int32_t* flags;               // may be null
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride, dq_stride, dk_stride;
+  int32_t T, Hq, Hkv, D, rotary_dim, max_positions;
+  int32_t units, units_per_token;
+  float eps;
+  bool f32, adjacent;
+};
+constexpr int kNormRopeMaxBlocks = 1024;   // workgroups of a backward call, each of which leaves a partial sum of dw
+hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t st);
+hipError_t launch_qk_norm_rope_backward(const NormRopeArgs& a, hipStream_t st);
+
 }  // namespace marl

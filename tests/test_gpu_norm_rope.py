@@ -1,0 +1,201 @@
+"""Norm of query / key heads with the rotation by position, forward and backward, against 64 bits.
+
+Tolerances, from the formulas: a row's sum of squares is at most 8 + 5 roundings deep, of which the reciprocal root keeps half, and
+has 2 of its own; the weight, the angle and the two products add 5: 16 units of 2^-24 of the magnitudes that are added up, taken as
+24.  Backward the mean of g n adds as many (taken as 48), and a sum of dw is at most 4 + 2 + 4 + 64 additions deep for the rows of
+these tests (taken as 128).  A bf16 result is rounded once more: 2^-8 of its value (half of it by rounding to nearest, half for the
+case that the float32 value lies on the other side of a tie)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_09578_amd import binding as B
+from tests import norm_rope_ref as ref
+
+pytestmark = pytest.mark.gpu
+EPS32 = 2.0 ** -24
+EPS = 1e-6
+MAX_POS = 4096
+
+
+def make(T, Hq, Hkv, D, rot, dtype, seed, layout="fused", weights=True):
+    g = torch.Generator().manual_seed(seed)
+    rnd = lambda *s: torch.randn(*s, generator=g)
+    fused = (rnd(T, (Hq + 2 * Hkv) * D) * torch.exp(rnd(T, 1))).to(dtype).cuda()
+    if layout == "fused":
+        q, k = fused[:, : Hq * D].view(T, Hq, D), fused[:, Hq * D: (Hq + Hkv) * D].view(T, Hkv, D)
+    else:
+        q, k = fused[:, : Hq * D].reshape(T, Hq, D).contiguous(), fused[:, Hq * D: (Hq + Hkv) * D].reshape(T, Hkv, D).contiguous()
+    d = dict(q=q, k=k, q_weight=(1 + 0.3 * rnd(D)).to(dtype).cuda() if weights else None,
+             k_weight=(1 + 0.3 * rnd(D)).to(dtype).cuda() if weights else None,
+             cos_sin=torch.from_numpy(ref.table(MAX_POS, rot)).cuda(), positions=torch.randint(0, MAX_POS, (T,), generator=g).int().cuda(),
+             dq_out=rnd(T, Hq, D).to(dtype).cuda(), dk_out=rnd(T, Hkv, D).to(dtype).cuda())
+    if T > 2:
+        d["q"][1, 0] = 0.0          # a row of zeros
+        d["k"][2] *= 1e-4           # one that eps weighs on
+    return d
+
+
+def f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def weight(d, n, D):
+    return np.ones(D) if d[n] is None else f64(d[n])
+
+
+def close(got, want, magnitude, units, dtype):
+    allowed = units * EPS32 * magnitude + (2.0 ** -8 * np.abs(want) if dtype == torch.bfloat16 else 0.0) + 1e-37
+    worst = np.max(np.abs(f64(got) - want) / allowed) if want.size else 0.0
+    assert worst <= 1.0, f"{worst} of the tolerance"
+
+
+CASES = [  # T, Hq, Hkv, D, rot, adjacent, dtype
+    (1, 8, 2, 128, 128, False, torch.bfloat16), (1, 1, 1, 128, 128, False, torch.bfloat16), (5, 28, 4, 128, 128, False, torch.bfloat16),
+    (64, 64, 8, 128, 128, False, torch.bfloat16), (333, 8, 2, 128, 64, True, torch.float32), (77, 16, 1, 128, 32, False, torch.bfloat16),
+    (9, 3, 5, 128, 16, False, torch.float32), (131, 7, 7, 64, 64, False, torch.bfloat16), (50, 9, 3, 64, 32, True, torch.bfloat16),
+    (33, 12, 1, 64, 48, False, torch.float32), (41, 5, 2, 256, 256, False, torch.bfloat16), (23, 4, 4, 256, 64, True, torch.float32),
+    (17, 32, 8, 256, 112, False, torch.float32), (29, 28, 4, 128, 0, False, torch.bfloat16), (8, 2, 1, 64, 0, True, torch.float32),
+    (700, 28, 4, 128, 128, False, torch.bfloat16), (520, 64, 8, 128, 128, True, torch.float32), (300, 64, 8, 64, 64, False, torch.bfloat16),
+    (4200, 8, 2, 128, 128, False, torch.bfloat16), (1100, 28, 4, 64, 32, True, torch.float32), (1030, 13, 3, 256, 128, False, torch.bfloat16)]
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,D,rot,adjacent,dtype", CASES)
+@pytest.mark.parametrize("layout", ["fused", "apart"])
+def test_forward(T, Hq, Hkv, D, rot, adjacent, dtype, layout):
+    print("case: norm rope", T, Hq, Hkv, D, rot, adjacent, dtype, layout, flush=True)
+    d = make(T, Hq, Hkv, D, rot, dtype, T + D, layout)
+    M = ref.rotation(f64(d["cos_sin"]), d["positions"].cpu().numpy(), D, adjacent)
+    flags = torch.zeros(1, dtype=torch.int32, device="cuda")
+    q_out, k_out = torch.empty(T, Hq, D, dtype=dtype, device="cuda"), torch.empty(T, Hkv, D, dtype=dtype, device="cuda")
+    B.marl_qk_norm_rope(d["q"], d["k"], d["q_weight"], d["k_weight"], d["cos_sin"], d["positions"], EPS, q_out, k_out, adjacent, flags)
+    for got, n in ((q_out, "q"), (k_out, "k")):
+        want, magnitude = ref.forward(f64(d[n]), f64(d[n + "_weight"]), M, EPS)
+        close(got, want, magnitude, 24, dtype)
+    assert int(flags) == 0
+    # in place, into the fused array or the arrays themselves: the same bits
+    B.marl_qk_norm_rope(d["q"], d["k"], d["q_weight"], d["k_weight"], d["cos_sin"], d["positions"], EPS, d["q"], d["k"], adjacent)
+    assert torch.equal(d["q"], q_out) and torch.equal(d["k"], k_out)
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,D,rot,adjacent,dtype", CASES)
+def test_backward(T, Hq, Hkv, D, rot, adjacent, dtype):
+    print("case: norm rope backward", T, Hq, Hkv, D, rot, adjacent, dtype, flush=True)
+    d = make(T, Hq, Hkv, D, rot, dtype, 7 * T + D)
+    M = ref.rotation(f64(d["cos_sin"]), d["positions"].cpu().numpy(), D, adjacent)
+    ws = B.alloc_workspace(B.marl_qk_norm_rope_workspace_bytes(T, Hq, Hkv, D), "cuda")
+    ws.fill_(0xFF)
+    dfused = torch.full((T, (Hq + 2 * Hkv) * D), 7.0, dtype=dtype, device="cuda")     # the projection's gradient, values' part untouched
+    dq, dk = dfused[:, : Hq * D].view(T, Hq, D), dfused[:, Hq * D: (Hq + Hkv) * D].view(T, Hkv, D)
+    dqw, dkw = (torch.full((D,), float("nan"), device="cuda") for _ in range(2))
+    call = lambda o: B.marl_qk_norm_rope_backward(d["dq_out"], d["dk_out"], d["q"], d["k"], d["q_weight"], d["k_weight"], d["cos_sin"],
+                                                  d["positions"], EPS, *o, ws, adjacent)
+    call((dq, dk, dqw, dkw))
+    for n, dx, dw in (("q", dq, dqw), ("k", dk, dkw)):
+        want, want_w, mag, mag_w = ref.backward(f64(d["d" + n + "_out"]), f64(d[n]), f64(d[n + "_weight"]), M, EPS)
+        close(dx, want, mag, 48, dtype)
+        close(dw, want_w, mag_w, 128, torch.float32)
+    assert bool((dfused[:, (Hq + Hkv) * D:] == 7).all())
+    # again, in place of the incoming gradients and without dk's weights: the same bits
+    dqw2 = torch.empty(D, device="cuda")
+    call((d["dq_out"], d["dk_out"], dqw2, None))
+    assert torch.equal(d["dq_out"], dq) and torch.equal(d["dk_out"], dk) and torch.equal(dqw2, dqw)
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_gradient_against_differences(adjacent):
+    """<dx, v> + <dw, u> is the derivative of <dz, z> along (v, u): central differences of the 64-bit forward pass."""
+    T, Hq, Hkv, D, rot = 6, 4, 2, 128, 64
+    d = make(T, Hq, Hkv, D, rot, torch.float32, 11)
+    M = ref.rotation(f64(d["cos_sin"]), d["positions"].cpu().numpy(), D, adjacent)
+    ws = B.alloc_workspace(B.marl_qk_norm_rope_workspace_bytes(T, Hq, Hkv, D), "cuda")
+    out = [torch.empty_like(d["dq_out"]), torch.empty_like(d["dk_out"]), torch.empty(D, device="cuda"), torch.empty(D, device="cuda")]
+    B.marl_qk_norm_rope_backward(d["dq_out"], d["dk_out"], d["q"], d["k"], d["q_weight"], d["k_weight"], d["cos_sin"], d["positions"], EPS, *out, ws, adjacent)
+    rng = np.random.default_rng(3)
+    for n, dx, dw in (("q", out[0], out[2]), ("k", out[1], out[3])):
+        x, w, dz = f64(d[n]), f64(d[n + "_weight"]), f64(d["d" + n + "_out"])
+        v, u = rng.standard_normal(x.shape) * np.abs(x).mean(-1, keepdims=True), rng.standard_normal(w.shape)
+        f = lambda h: (dz * ref.forward(x + h * v, w + h * u, M, EPS)[0]).sum()
+        h = 1e-5
+        terms = np.abs(f64(dx) * v).sum() + np.abs(f64(dw) * u).sum()
+        # 2^-24 of the terms for each of up to 128 roundings, and 1e-6 of them for the differences
+        assert abs((f(h) - f(-h)) / (2 * h) - (f64(dx) * v).sum() - (f64(dw) * u).sum()) <= (128 * EPS32 + 1e-6) * terms
+
+
+def test_no_weights_no_eps_and_repeated_inputs():
+    """Unit weights; eps 0; one token's row read for every token (stride 0) and gradients written apart."""
+    T, Hq, Hkv, D = 37, 6, 2, 128
+    d = make(T, Hq, Hkv, D, 128, torch.float32, 4, weights=False)
+    M = ref.rotation(f64(d["cos_sin"]), d["positions"].cpu().numpy(), D, False)
+    q, k = d["q"][5:6].expand(T, Hq, D), d["k"][5:6].expand(T, Hkv, D)
+    q_out, k_out = torch.empty(T, Hq, D, device="cuda"), torch.empty(T, Hkv, D, device="cuda")
+    B.marl_qk_norm_rope(q, k, None, None, d["cos_sin"], d["positions"], 0.0, q_out, k_out)
+    ws = B.alloc_workspace(B.marl_qk_norm_rope_workspace_bytes(T, Hq, Hkv, D), "cuda")
+    dq, dk, dqw, dkw = torch.empty_like(q_out), torch.empty_like(k_out), torch.empty(D, device="cuda"), torch.empty(D, device="cuda")
+    B.marl_qk_norm_rope_backward(d["dq_out"], d["dk_out"], q, k, None, None, d["cos_sin"], d["positions"], 0.0, dq, dk, dqw, dkw, ws)
+    for x, z, dz, dx, dw in ((q, q_out, d["dq_out"], dq, dqw), (k, k_out, d["dk_out"], dk, dkw)):
+        want, mag = ref.forward(f64(x), np.ones(D), M, 0.0)
+        close(z, want, mag, 24, torch.float32)
+        want, want_w, mag, mag_w = ref.backward(f64(dz), f64(x), np.ones(D), M, 0.0)
+        close(dx, want, mag, 48, torch.float32)
+        close(dw, want_w, mag_w, 128, torch.float32)
+
+
+def test_positions_outside_the_table_and_no_tokens():
+    T, Hq, Hkv, D = 4, 2, 1, 128
+    d = make(T, Hq, Hkv, D, 128, torch.float32, 9)
+    flags = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = lambda: (torch.empty(T, Hq, D, device="cuda"), torch.empty(T, Hkv, D, device="cuda"))
+    bad, near = torch.tensor([3, -7, MAX_POS, 2 ** 31 - 1]).int().cuda(), torch.tensor([3, 0, MAX_POS - 1, MAX_POS - 1]).int().cuda()
+    a, b = out(), out()
+    B.marl_qk_norm_rope(d["q"], d["k"], None, None, d["cos_sin"], bad, EPS, *a, flags=flags)
+    assert int(flags) == B.FLAG_BAD_POSITION
+    flags.zero_()
+    B.marl_qk_norm_rope(d["q"], d["k"], None, None, d["cos_sin"], near, EPS, *b, flags=flags)
+    assert int(flags) == 0 and torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    none = torch.empty(0, Hq, D, device="cuda"), torch.empty(0, Hkv, D, device="cuda")
+    pos = torch.empty(0, dtype=torch.int32, device="cuda")
+    B.marl_qk_norm_rope(*none, None, None, d["cos_sin"], pos, EPS, *none)
+    ws = B.alloc_workspace(B.marl_qk_norm_rope_workspace_bytes(0, Hq, Hkv, D), "cuda")
+    dqw, dkw = torch.full((D,), 3.0, device="cuda"), torch.full((D,), 3.0, device="cuda")
+    B.marl_qk_norm_rope_backward(*none, *none, None, None, d["cos_sin"], pos, EPS, *none, dqw, dkw, ws)
+    assert not dqw.any() and not dkw.any()
+
+
+def test_infinities_stay_in_their_rows():
+    d = make(20, 8, 2, 128, 128, torch.bfloat16, 2)
+    outs = []
+    for poison in (False, True):
+        if poison:
+            d["q"][3, 5, 17], d["q"][7, 2, 100], d["k"][9, 1, 0] = float("inf"), float("nan"), -float("inf")
+        outs.append((torch.empty_like(d["dq_out"]), torch.empty_like(d["dk_out"])))
+        B.marl_qk_norm_rope(d["q"], d["k"], d["q_weight"], d["k_weight"], d["cos_sin"], d["positions"], EPS, *outs[-1])
+    for a, b, rows in ((outs[0][0], outs[1][0], [(3, 5), (7, 2)]), (outs[0][1], outs[1][1], [(9, 1)])):
+        same = (a == b).all(-1).cpu()
+        for r in rows:
+            same[r] = True
+        assert bool(same.all())
+
+
+def test_another_stream_and_bad_tensors():
+    d = make(40, 8, 2, 128, 128, torch.bfloat16, 8)
+    want = torch.empty_like(d["dq_out"]), torch.empty_like(d["dk_out"])
+    args = d["q"], d["k"], d["q_weight"], d["k_weight"], d["cos_sin"], d["positions"], EPS
+    B.marl_qk_norm_rope(*args, *want)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got = torch.zeros_like(want[0]), torch.zeros_like(want[1])
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        B.marl_qk_norm_rope(*args, *got)
+    s.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for k, w in ((0, d["q"].float()), (0, d["q"][:-1]), (1, d["k"].transpose(0, 1)), (2, d["q_weight"].float()), (2, d["q_weight"][:-1]),
+                 (4, d["cos_sin"].double()), (5, d["positions"].long()), (5, d["positions"][:-1]), (5, None), (1, d["k"].cpu()),
+                 (0, d["q"].transpose(1, 2).contiguous().transpose(1, 2))):
+        bad = list(args)
+        bad[k] = w
+        with pytest.raises(ValueError):
+            B.marl_qk_norm_rope(*bad, *want)
+    with pytest.raises(B.MarlError):
+        B.marl_qk_norm_rope(*args, want[0][:1].expand(40, 8, 128), want[1])     # results on top of each other
