@@ -346,6 +346,36 @@ int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, con
                          void* stream);
 
 /*
+ * KV cache in 8 bits: half the bytes of a bf16 one, so twice the samples on a GPU and half the time of a decode step that is bound by
+ * reading them.  A token's key or value of one KV head, a row of 128 numbers, is stored as 128 e4m3 codes (1 sign, 4 exponent bits of
+ * bias 7, 3 mantissa bits; no infinities, 0x7f and 0xff are NaN) and one exponent e, and stands for code * 2^e:
+ *   k_pages    e4m3 [num_pages, Hkv, 16 slots, 128]    v_pages    e4m3 [num_pages, Hkv, 128, 16 slots]    (as in the bf16 cache)
+ *   exponents  int8 [num_pages, Hkv, 2, 16]            (0: of the keys, 1: of the values)
+ * Writing a bf16 row chooses the smallest e >= -110 with max |x| <= 448 * 2^e over the row's finite numbers (-110 if all are zero)
+ * and rounds x / 2^e to the nearest code, ties to even: at most 2^-4 off, relatively, above 2^(e - 6), and 2^(e - 10) below.  With
+ * e = 120 codes end at 240, as 256 * 2^120 is no bf16 number any more.  Infinities become the largest code, NaN stays NaN.  Every value that a
+ * stored row stands for is exactly a bf16 number.
+ *
+ * marl_kv_append_fp8 and marl_kv_write_prompt_fp8 are marl_kv_append and marl_kv_write_prompt into such a cache: the same
+ * arguments, limits and flags, and `exponents`.  All arrays that they and the calls below read or write in vectors
+ * (k_new, v_new, pages and exponents) must be 16-byte aligned (MARL_INVALID_ARG otherwise).
+ *
+ * marl_kv_read_pages_fp8: for i < n, bf16 page dst[i] of k_pages / v_pages (num_out_pages pages, as in marl_decode_attn) becomes what 8-bit page
+ * src[i] stands for, all KV heads, keys and values, slots that no token owns included: for calls that take a bf16 cache, such
+ * as marl_prefill_attn for a further chunk of a prompt.  src, dst: device int32 [n]; a dst must not appear twice in a call.  Pairs with
+ * an id outside [0, num_pages) or [0, num_out_pages) are skipped and flagged (MARL_FLAG_BAD_PAGE in *flags, which may be NULL).
+ */
+int marl_kv_append_fp8(const marl_attn_shape* shape, const void* k_new, const void* v_new,
+                       void* k_pages, void* v_pages, int8_t* exponents, const int32_t* suffix_block_table,
+                       int32_t* suffix_lens, int32_t* flags, void* stream);
+int marl_kv_write_prompt_fp8(const marl_prefill_shape* shape, const void* k_new, const void* v_new,
+                             void* k_pages, void* v_pages, int8_t* exponents, const int32_t* prefix_block_table,
+                             const int32_t* q_start, const int32_t* q_pos0, int32_t* flags, void* stream);
+int marl_kv_read_pages_fp8(int32_t num_kv_heads, int32_t num_pages, const void* k_codes, const void* v_codes,
+                           const int8_t* exponents, int32_t num_out_pages, void* k_pages, void* v_pages,
+                           const int32_t* src, const int32_t* dst, int32_t n, int32_t* flags, void* stream);
+
+/*
  * Group-normalised advantages of GRPO (Shao et al. 2024; the paper trains every agent with
  * GRPO, Section 8.1).  For each group g (the samples of one prompt) with members
  * group_seqs[group_start[g] .. group_start[g+1]):

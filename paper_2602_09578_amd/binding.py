@@ -171,6 +171,10 @@ def load_library(build_if_missing: bool = True):
     lib.marl_pack_tensors.argtypes = [VP, I32, ctypes.c_int64, VP, VP]
     lib.marl_unpack_tensors.argtypes = [VP, I32, ctypes.c_int64, VP, VP]
     lib.marl_pack_plan.restype = lib.marl_pack_tensors.restype = lib.marl_unpack_tensors.restype = ctypes.c_int
+    lib.marl_kv_append_fp8.argtypes = [PS] + [VP] * 9
+    lib.marl_kv_write_prompt_fp8.argtypes = [PP] + [VP] * 10
+    lib.marl_kv_read_pages_fp8.argtypes = [I32, I32, VP, VP, VP, I32, VP, VP, VP, VP, I32, VP, VP]
+    lib.marl_kv_append_fp8.restype = lib.marl_kv_write_prompt_fp8.restype = lib.marl_kv_read_pages_fp8.restype = ctypes.c_int
     PN = ctypes.POINTER(NormRopeShape)
     lib.marl_qk_norm_rope.argtypes = [PN] + [VP] * 10
     lib.marl_qk_norm_rope_workspace_bytes.argtypes = [PN, ctypes.POINTER(SZ)]
@@ -518,6 +522,74 @@ def marl_kv_write_prompt(shape: PrefillShape, k_new, v_new, k_pages, v_pages, pr
                                              _ptr(v_pages), _ptr(prefix_block_table), _ptr(q_start), _ptr(q_pos0),
                                              _ptr(flags) if flags is not None else None, _stream(k_new.device))
     _check(rc, "marl_kv_write_prompt")
+
+
+# ---- KV cache in 8 bits (layout and rounding: see the header) ------------------------------------
+FP8 = torch.float8_e4m3fn
+
+
+def alloc_kv_fp8(num_pages: int, num_kv_heads: int, device):
+    """(k_pages, v_pages, exponents) of an 8-bit cache, zeros."""
+    return (torch.zeros(num_pages, num_kv_heads, 16, 128, dtype=torch.uint8, device=device).view(FP8),
+            torch.zeros(num_pages, num_kv_heads, 128, 16, dtype=torch.uint8, device=device).view(FP8),
+            torch.zeros(num_pages, num_kv_heads, 2, 16, dtype=torch.int8, device=device))
+
+
+def _require_fp8_cache(num_pages, Hkv, k_pages, v_pages, exponents):
+    _require(k_pages, "k_pages", FP8, (num_pages, Hkv, 16, 128))
+    _require(v_pages, "v_pages", FP8, (num_pages, Hkv, 128, 16))
+    _require(exponents, "exponents", torch.int8, (num_pages, Hkv, 2, 16))
+    _require_cuda(k_pages, v_pages, exponents)
+
+
+def marl_kv_append_fp8(shape: AttnShape, k_new, v_new, k_pages, v_pages, exponents, suffix_block_table, suffix_lens,
+                       flags: Optional[torch.Tensor] = None):
+    """marl_kv_append into an 8-bit cache."""
+    NS, Hkv = shape.num_seqs, shape.num_kv_heads
+    _require_cuda(k_new, v_new, suffix_block_table, suffix_lens, flags)
+    _require_fp8_cache(shape.num_pages, Hkv, k_pages, v_pages, exponents)
+    _require(k_new, "k_new", torch.bfloat16, (NS, Hkv, 128))
+    _require(v_new, "v_new", torch.bfloat16, (NS, Hkv, 128))
+    _require(suffix_block_table, "suffix_block_table", torch.int32, (NS, shape.max_suffix_pages))
+    _require(suffix_lens, "suffix_lens", torch.int32, (NS,))
+    _require(flags, "flags", torch.int32)
+    rc = load_library().marl_kv_append_fp8(ctypes.byref(shape), _ptr(k_new), _ptr(v_new), _ptr(k_pages), _ptr(v_pages), _ptr(exponents),
+                                           _ptr(suffix_block_table), _ptr(suffix_lens), _ptr(flags), _stream(k_pages.device))
+    _check(rc, "marl_kv_append_fp8")
+
+
+def marl_kv_write_prompt_fp8(shape: PrefillShape, k_new, v_new, k_pages, v_pages, exponents, prefix_block_table, q_start, q_pos0,
+                             flags: Optional[torch.Tensor] = None):
+    """marl_kv_write_prompt into an 8-bit cache."""
+    NT, NG, Hkv = shape.num_tokens, shape.num_groups, shape.num_kv_heads
+    _require_cuda(k_new, v_new, prefix_block_table, q_start, q_pos0, flags)
+    _require_fp8_cache(shape.num_pages, Hkv, k_pages, v_pages, exponents)
+    _require(k_new, "k_new", torch.bfloat16, (NT, Hkv, 128))
+    _require(v_new, "v_new", torch.bfloat16, (NT, Hkv, 128))
+    _require(prefix_block_table, "prefix_block_table", torch.int32, (NG, shape.max_prefix_pages))
+    _require(q_start, "q_start", torch.int32, (NG + 1,))
+    _require(q_pos0, "q_pos0", torch.int32, (NG,))
+    _require(flags, "flags", torch.int32)
+    rc = load_library().marl_kv_write_prompt_fp8(ctypes.byref(shape), _ptr(k_new), _ptr(v_new), _ptr(k_pages), _ptr(v_pages), _ptr(exponents),
+                                                 _ptr(prefix_block_table), _ptr(q_start), _ptr(q_pos0), _ptr(flags), _stream(k_new.device))
+    _check(rc, "marl_kv_write_prompt_fp8")
+
+
+def marl_kv_read_pages_fp8(k_codes, v_codes, exponents, src, dst, k_pages, v_pages, flags: Optional[torch.Tensor] = None):
+    """bf16 page dst[i] of k_pages / v_pages becomes what 8-bit page src[i] stands for."""
+    if k_codes.dim() != 4 or k_pages.dim() != 4:
+        raise ValueError("k_codes, k_pages: expected [pages, Hkv, 16, 128]")
+    pages, Hkv, out_pages, n = k_codes.shape[0], k_codes.shape[1], k_pages.shape[0], int(src.numel())
+    _require_fp8_cache(pages, Hkv, k_codes, v_codes, exponents)
+    _require(k_pages, "k_pages", torch.bfloat16, (out_pages, Hkv, 16, 128))
+    _require(v_pages, "v_pages", torch.bfloat16, (out_pages, Hkv, 128, 16))
+    _require(src, "src", torch.int32, (n,))
+    _require(dst, "dst", torch.int32, (n,))
+    _require(flags, "flags", torch.int32)
+    _require_cuda(src, dst, k_pages, v_pages, flags)
+    rc = load_library().marl_kv_read_pages_fp8(Hkv, pages, _ptr(k_codes), _ptr(v_codes), _ptr(exponents), out_pages, _ptr(k_pages),
+                                               _ptr(v_pages), _ptr(src), _ptr(dst), n, _ptr(flags), _stream(k_pages.device))
+    _check(rc, "marl_kv_read_pages_fp8")
 
 
 def prepare_prefill(inp, out_dtype=MARL_OUT_BF16):

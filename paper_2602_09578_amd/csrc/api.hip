@@ -463,6 +463,58 @@ int marl_kv_copy_pages(const marl_attn_shape* shape, void* k_pages, void* v_page
   return e == hipSuccess ? MARL_OK : hip_fail(e, "kv copy kernel");
 }
 
+// ---- 8-bit cache ----------------------------------------------------------------------------------
+int marl_kv_append_fp8(const marl_attn_shape* shape, const void* k_new, const void* v_new,
+                       void* k_pages, void* v_pages, int8_t* exponents, const int32_t* suffix_block_table,
+                       int32_t* suffix_lens, int32_t* flags, void* stream) {
+  const int rc = check_shape(shape);
+  if (rc != MARL_OK) return rc;
+  if (shape->num_seqs == 0) return MARL_OK;
+  if (!k_new || !v_new || !k_pages || !v_pages || !exponents || !suffix_block_table || !suffix_lens) return MARL_INVALID_ARG;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(exponents)) return MARL_INVALID_ARG;
+  if (shape->max_suffix_pages < 1) return MARL_INVALID_ARG;
+  marl::KvAppendFp8Args a;
+  a.k_new = static_cast<const uint16_t*>(k_new);
+  a.v_new = static_cast<const uint16_t*>(v_new);
+  a.k_pages = static_cast<uint8_t*>(k_pages);
+  a.v_pages = static_cast<uint8_t*>(v_pages);
+  a.exponents = exponents;
+  a.suffix_table = suffix_block_table;
+  a.suffix_lens = suffix_lens;
+  a.flags = flags;
+  a.NS = shape->num_seqs;
+  a.Hkv = shape->num_kv_heads;
+  a.num_pages = shape->num_pages;
+  a.max_sp = shape->max_suffix_pages;
+  const hipError_t e = marl::launch_kv_append_fp8(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? MARL_OK : hip_fail(e, "8-bit kv append kernel");
+}
+
+int marl_kv_read_pages_fp8(int32_t num_kv_heads, int32_t num_pages, const void* k_codes, const void* v_codes,
+                           const int8_t* exponents, int32_t num_out_pages, void* k_pages, void* v_pages,
+                           const int32_t* src, const int32_t* dst, int32_t n, int32_t* flags, void* stream) {
+  if (num_kv_heads < 1 || num_pages < 1 || num_out_pages < 1 || n < 0) return MARL_INVALID_ARG;
+  if ((long)n * num_kv_heads >= (1L << 31)) return MARL_UNSUPPORTED;   // one workgroup per page and KV head
+  if (n == 0) return MARL_OK;
+  if (!k_codes || !v_codes || !exponents || !k_pages || !v_pages || !src || !dst) return MARL_INVALID_ARG;
+  if (!aligned16(k_codes) || !aligned16(v_codes) || !aligned16(exponents) || !aligned16(k_pages) || !aligned16(v_pages)) return MARL_INVALID_ARG;
+  marl::KvReadFp8Args a;
+  a.k_codes = static_cast<const uint8_t*>(k_codes);
+  a.v_codes = static_cast<const uint8_t*>(v_codes);
+  a.exponents = exponents;
+  a.k_pages = static_cast<uint16_t*>(k_pages);
+  a.v_pages = static_cast<uint16_t*>(v_pages);
+  a.src = src;
+  a.dst = dst;
+  a.flags = flags;
+  a.n = n;
+  a.Hkv = num_kv_heads;
+  a.num_pages = num_pages;
+  a.num_out_pages = num_out_pages;
+  const hipError_t e = marl::launch_kv_read_pages_fp8(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? MARL_OK : hip_fail(e, "8-bit page read kernel");
+}
+
 // ---- log-probabilities ------------------------------------------------------------------------
 // How a call is divided: the slices that the caller's workspace is sized for, and whether the rows are taken whole all
 // the same.  Whole rows need no second kernel: short rows at any number (16 x 20481: 6.1 us in slices, 4.1 whole), up to
@@ -724,10 +776,10 @@ int marl_prefill_attn(const marl_prefill_shape* shape, void* workspace, size_t w
   return e == hipSuccess ? MARL_OK : hip_fail(e, "prefill kernels");
 }
 
-int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, const void* v_new,
-                         void* k_pages, void* v_pages, const int32_t* prefix_block_table,
-                         const int32_t* q_start, const int32_t* q_pos0, int32_t* flags,
-                         void* stream) {
+// `exponents`: of an 8-bit cache, null for a bf16 one.
+static int write_prompt(const marl_prefill_shape* shape, const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                        int8_t* exponents, const int32_t* prefix_block_table, const int32_t* q_start,
+                        const int32_t* q_pos0, int32_t* flags, void* stream) {
   const int rc = check_prefill_shape(shape);
   if (rc != MARL_OK) return rc;
   if (shape->num_tokens == 0 || shape->num_groups == 0) return MARL_OK;
@@ -742,14 +794,32 @@ int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, con
   fill_prefill_args(shape, a);
   a.k_new = static_cast<const uint16_t*>(k_new);
   a.v_new = static_cast<const uint16_t*>(v_new);
-  a.k_pages_w = static_cast<uint16_t*>(k_pages);
-  a.v_pages_w = static_cast<uint16_t*>(v_pages);
+  a.k_pages_w = k_pages;
+  a.v_pages_w = v_pages;
+  a.exponents_w = exponents;
   a.prefix_table = prefix_block_table;
   a.q_start = q_start;
   a.q_pos0 = q_pos0;
   a.flags = flags;
   const hipError_t e = marl::launch_kv_write_prompt(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? MARL_OK : hip_fail(e, "prompt scatter kernel");
+}
+
+int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, const void* v_new,
+                         void* k_pages, void* v_pages, const int32_t* prefix_block_table,
+                         const int32_t* q_start, const int32_t* q_pos0, int32_t* flags,
+                         void* stream) {
+  return write_prompt(shape, k_new, v_new, k_pages, v_pages, nullptr, prefix_block_table, q_start, q_pos0, flags, stream);
+}
+
+int marl_kv_write_prompt_fp8(const marl_prefill_shape* shape, const void* k_new, const void* v_new,
+                             void* k_pages, void* v_pages, int8_t* exponents, const int32_t* prefix_block_table,
+                             const int32_t* q_start, const int32_t* q_pos0, int32_t* flags, void* stream) {
+  const int rc = check_prefill_shape(shape);
+  if (rc != MARL_OK) return rc;
+  if (shape->num_tokens == 0 || shape->num_groups == 0) return MARL_OK;
+  if (!exponents || !aligned16(exponents) || !aligned16(v_new)) return MARL_INVALID_ARG;   // (rows of both are read as vectors here)
+  return write_prompt(shape, k_new, v_new, k_pages, v_pages, exponents, prefix_block_table, q_start, q_pos0, flags, stream);
 }
 
 // ---- GRPO advantages ----------------------------------------------------------------------------

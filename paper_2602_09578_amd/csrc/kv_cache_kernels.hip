@@ -3,12 +3,14 @@
 // another one.  The paper only says that rollout manages large KV caches (Section 4.1) and
 // that prompts are expanded into several samples (Section 5.1); the operations are the
 // plain scatter / copy stated in marl_decode.h.  Pure data movement: results are bit-exact.
+//   Into an 8-bit cache (kv_fp8.h) the appended rows are quantised on their way, and whole pages are read back as bf16, for
+// calls that take a bf16 cache (a further chunk of a prompt).
+#include "kv_fp8.h"
 #include "marl_internal.h"
+#include "wave_ops.h"
 
 namespace marl {
 namespace {
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // One workgroup of 256 threads per sequence: a thread stores V channels (2 bytes each, the layout keeps
 // a channel's 16 slots together) of up to four (head, channel) pairs at a time and one 16-byte piece of
@@ -54,6 +56,74 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(KvAppendArgs 
   if (page >= 0 && tid == 0) a.suffix_lens[s] = pos + 1;
 }
 
+// The append of an 8-bit cache.  16 lanes take a row (8 channels each), so 256 threads the keys and values of eight heads at a time.
+// The codes of a key are contiguous; those of a value lie 16 bytes apart, one byte per channel.
+__global__ __launch_bounds__(kAppendThreads) void kv_append_fp8_kernel(KvAppendFp8Args a) {
+  constexpr int kHeads = kAppendThreads / 32;
+  const int s = blockIdx.x;
+  const int piece = threadIdx.x & 15, which = threadIdx.x >> 7, head = (threadIdx.x >> 4) & (kHeads - 1);
+  const int pos = a.suffix_lens[s];
+  const uint16_t* rows = (which ? a.v_new : a.k_new) + ((size_t)s * a.Hkv) * kD + piece * 8;
+  int flag = 0;
+  int page = -1;
+  if (pos < 0 || pos >= a.max_sp * kPage) flag = MARL_FLAG_LEN_CLAMPED;          // no room in the table row
+  else {
+    page = a.suffix_table[(size_t)s * a.max_sp + (pos >> 4)];
+    if ((unsigned)page >= (unsigned)a.num_pages) { flag = MARL_FLAG_BAD_PAGE; page = -1; }
+  }
+  const int slot = pos & (kPage - 1);
+  for (int h0 = 0; h0 < a.Hkv; h0 += kHeads) {                                   // workgroup-uniform
+    const int h = h0 + head;
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if (h < a.Hkv) w = *reinterpret_cast<const u32x4*>(rows + (size_t)h * kD);
+    int e;
+    const u32x2 codes = quantize_row(w, e);
+    if (page < 0 || h >= a.Hkv) continue;
+    const size_t row = (size_t)page * a.Hkv + h;
+    if (which == 0) {
+      *reinterpret_cast<u32x2*>(a.k_pages + row * (kPage * kD) + slot * kD + piece * 8) = codes;
+    } else {
+      uint8_t* at = a.v_pages + row * (kPage * kD) + piece * 8 * kPage + slot;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) at[i * kPage] = (uint8_t)(codes[i >> 2] >> (8 * (i & 3)));
+    }
+    if (piece == 0) a.exponents[row * (2 * kPage) + which * kPage + slot] = (int8_t)e;
+  }
+  if (flag && threadIdx.x == 0 && a.flags) atomicOr(a.flags, flag);
+  __syncthreads();
+  if (page >= 0 && threadIdx.x == 0) a.suffix_lens[s] = pos + 1;
+}
+
+// bf16 page dst[i] <- 8-bit page src[i]: one workgroup per (pair, KV head), a thread for eight codes of the keys and eight of the
+// values, so that a wave stores 1 KB at a time.  The exponents of eight neighbouring slots of a value row are one load.
+__global__ __launch_bounds__(256) void kv_read_pages_fp8_kernel(KvReadFp8Args a) {
+  const int pair = blockIdx.x / a.Hkv, h = blockIdx.x - pair * a.Hkv, t = threadIdx.x;
+  const int src = a.src[pair], dst = a.dst[pair];
+  if ((unsigned)src >= (unsigned)a.num_pages || (unsigned)dst >= (unsigned)a.num_out_pages) {
+    if (t == 0 && a.flags) atomicOr(a.flags, MARL_FLAG_BAD_PAGE);
+    return;
+  }
+  const size_t from = (size_t)src * a.Hkv + h, to = ((size_t)dst * a.Hkv + h) * (kPage * kD) + t * 8;
+  const int8_t* ex = a.exponents + from * (2 * kPage);
+  const u32x2 k = *reinterpret_cast<const u32x2*>(a.k_codes + from * (kPage * kD) + t * 8);
+  const u32x2 v = *reinterpret_cast<const u32x2*>(a.v_codes + from * (kPage * kD) + t * 8);
+  const int ke = ex[t >> 4];
+  const u32x2 ve = *reinterpret_cast<const u32x2*>(ex + kPage + (t & 1) * 8);
+  u32x4 ko, vo;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const float ks = pow2(max(ke, -126));
+    ko[2 * i] = codes_to_bf16<false>(k[i], ks);
+    ko[2 * i + 1] = codes_to_bf16<true>(k[i], ks);
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[i], true);
+    vo[2 * i] = pack_bf16(__builtin_amdgcn_ldexpf(lo[0], exponent_of(ve[i], 0)), __builtin_amdgcn_ldexpf(lo[1], exponent_of(ve[i], 1)));
+    vo[2 * i + 1] = pack_bf16(__builtin_amdgcn_ldexpf(hi[0], exponent_of(ve[i], 2)), __builtin_amdgcn_ldexpf(hi[1], exponent_of(ve[i], 3)));
+  }
+  *reinterpret_cast<u32x4*>(a.k_pages + to) = ko;
+  *reinterpret_cast<u32x4*>(a.v_pages + to) = vo;
+}
+
 // dst[i] <- src[i] for whole pages (all KV heads, K and V): one workgroup per (pair, K|V)
 __global__ __launch_bounds__(256) void kv_copy_pages_kernel(KvCopyArgs a) {
   const int pair = blockIdx.x >> 1;
@@ -75,6 +145,18 @@ __global__ __launch_bounds__(256) void kv_copy_pages_kernel(KvCopyArgs a) {
 hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st) {
   if (a.NS == 0) return hipSuccess;
   hipLaunchKernelGGL(kv_append_kernel, dim3((unsigned)a.NS), dim3(kAppendThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_append_fp8(const KvAppendFp8Args& a, hipStream_t st) {
+  if (a.NS == 0) return hipSuccess;
+  hipLaunchKernelGGL(kv_append_fp8_kernel, dim3((unsigned)a.NS), dim3(kAppendThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_read_pages_fp8(const KvReadFp8Args& a, hipStream_t st) {
+  if (a.n == 0) return hipSuccess;
+  hipLaunchKernelGGL(kv_read_pages_fp8_kernel, dim3((unsigned)(a.n * a.Hkv)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -87,6 +87,31 @@ struct KvCopyArgs {
   int32_t* flags;   // may be null
   int32_t n, Hkv, num_pages;
 };
+// The same into an 8-bit cache (kv_fp8.h).
+struct KvAppendFp8Args {
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+  int8_t* exponents;   // [page][KV head][keys, values][slot]
+  const int32_t* suffix_table;
+  int32_t* suffix_lens;
+  int32_t* flags;      // may be null
+  int32_t NS, Hkv, num_pages, max_sp;
+};
+struct KvReadFp8Args {
+  const uint8_t* k_codes;
+  const uint8_t* v_codes;
+  const int8_t* exponents;
+  uint16_t* k_pages;
+  uint16_t* v_pages;
+  const int32_t* src;
+  const int32_t* dst;
+  int32_t* flags;      // may be null
+  int32_t n, Hkv, num_pages, num_out_pages;
+};
+hipError_t launch_kv_append_fp8(const KvAppendFp8Args& a, hipStream_t st);
+hipError_t launch_kv_read_pages_fp8(const KvReadFp8Args& a, hipStream_t st);
 hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st);
 hipError_t launch_kv_copy_pages(const KvCopyArgs& a, hipStream_t st);
 
@@ -151,8 +176,9 @@ struct PrefillArgs {
   // the prompt scatter only:
   const uint16_t* k_new;        // [NT][Hkv][128]
   const uint16_t* v_new;
-  uint16_t* k_pages_w;
-  uint16_t* v_pages_w;
+  void* k_pages_w;              // bf16, or codes where there are exponents
+  void* v_pages_w;
+  int8_t* exponents_w;          // of an 8-bit cache, else null
   int32_t* flags;
   int32_t NT, NG, Hq, Hkv, R, num_pages, max_pp, out_dtype, max_blocks;
   int32_t inv_R;                // ceil(65536 / R)

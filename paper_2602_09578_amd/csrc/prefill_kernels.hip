@@ -58,6 +58,7 @@
 // (6.59 M) and 5 % less time (3.63 and 3.44 ms on one card): what the traffic takes is power, and with it 0.1 GHz.
 #include <algorithm>
 
+#include "kv_fp8.h"
 #include "marl_internal.h"
 #include "wave_ops.h"
 
@@ -943,7 +944,7 @@ void prefill_small_kernel(PrefillArgs a) {
 // (4 KB): 16-byte copies.  Values are stored channel-major, so thread c collects channel c of the page's 16 tokens and writes
 // its 32 bytes with two stores when the chunk covers the whole page, else slot by slot.
 // What bounds it: memory (256 prompts, 1.36 GB read and written: 274 us, 5 TB/s), a short call its launch and three dependent reads.
-__device__ __forceinline__ void write_prompt_page(const PrefillArgs& a, const int g, const int b, const int n, const int pos0,
+__device__ __forceinline__ void write_prompt_page_bf16(const PrefillArgs& a, const int g, const int b, const int n, const int pos0,
                                                   const int kvh, const int col) {
   const int c = threadIdx.x;
   const int lo = max(pos0, col * kPage), hi = min(pos0 + n, (col + 1) * kPage);   // positions to write
@@ -953,6 +954,8 @@ __device__ __forceinline__ void write_prompt_page(const PrefillArgs& a, const in
     return;
   }
   const size_t blk = ((size_t)page * a.Hkv + kvh) * (kPage * kD);                 // elements
+  uint16_t* const k_pages = static_cast<uint16_t*>(a.k_pages_w);
+  uint16_t* const v_pages = static_cast<uint16_t*>(a.v_pages_w);
   const size_t tok0 = (size_t)b + (col * kPage - pos0);                           // token of slot 0 (may be "negative")
   const size_t row_stride = (size_t)a.Hkv * kD;
   // keys: 16 slots x 16 chunks of 16 bytes, two per thread
@@ -962,7 +965,7 @@ __device__ __forceinline__ void write_prompt_page(const PrefillArgs& a, const in
     const int slot = v >> 4, chunk = v & 15;
     const int pos = col * kPage + slot;
     if (pos >= lo && pos < hi)
-      *reinterpret_cast<u32x4*>(a.k_pages_w + blk + (size_t)slot * kD + chunk * 8) =
+      *reinterpret_cast<u32x4*>(k_pages + blk + (size_t)slot * kD + chunk * 8) =
           *reinterpret_cast<const u32x4*>(a.k_new + (tok0 + slot) * row_stride + (size_t)kvh * kD + chunk * 8);
   }
   // values: channel c of every slot
@@ -972,7 +975,7 @@ __device__ __forceinline__ void write_prompt_page(const PrefillArgs& a, const in
     const int pos = col * kPage + slot;
     vals[slot] = (pos >= lo && pos < hi) ? a.v_new[(tok0 + slot) * row_stride + (size_t)kvh * kD + c] : (uint16_t)0;
   }
-  uint16_t* vdst = a.v_pages_w + blk + (size_t)c * kPage;
+  uint16_t* vdst = v_pages + blk + (size_t)c * kPage;
   if (hi - lo == kPage) {
     u32x4 w0, w1;
 #pragma unroll
@@ -991,9 +994,87 @@ __device__ __forceinline__ void write_prompt_page(const PrefillArgs& a, const in
   }
 }
 
+// The same into an 8-bit cache (kv_fp8.h).  16 lanes take a row, 8 channels each, so a thread has two pieces of the keys and two of the
+// values; those of a page are quantised first, and the codes of the values turned in LDS: thread c collects channel c's 16 bytes.
+struct PromptCodes {
+  __attribute__((aligned(8))) uint8_t v[kPage][kD + 8];   // (rows 34 words apart: 16 lanes' pieces of four rows meet in two banks at most)
+};
+__device__ __forceinline__ void write_prompt_page_fp8(const PrefillArgs& a, const int g, const int b, const int n, const int pos0,
+                                                      const int kvh, const int col, PromptCodes& codes) {
+  const int c = threadIdx.x;
+  const int lo = max(pos0, col * kPage), hi = min(pos0 + n, (col + 1) * kPage);   // positions to write
+  const int page = a.prefix_table[(size_t)g * a.max_pp + col];
+  if ((unsigned)page >= (unsigned)a.num_pages) {                                  // workgroup-uniform
+    if (kvh == 0 && c == 0 && a.flags) atomicOr(a.flags, MARL_FLAG_BAD_PAGE);
+    return;
+  }
+  const size_t row = (size_t)page * a.Hkv + kvh;
+  uint8_t* const k_pages = static_cast<uint8_t*>(a.k_pages_w) + row * (kPage * kD);
+  uint8_t* const v_pages = static_cast<uint8_t*>(a.v_pages_w) + row * (kPage * kD);
+  int8_t* const exponents = a.exponents_w + row * (2 * kPage);
+  const size_t tok0 = (size_t)b + (col * kPage - pos0);                           // token of slot 0 (may be "negative")
+  const int piece = c & 15;
+  u32x4 k[2], v[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int slot = (c >> 4) + 8 * u, pos = col * kPage + slot;
+    k[u] = v[u] = u32x4{0u, 0u, 0u, 0u};
+    if (pos >= lo && pos < hi) {
+      const size_t at = ((tok0 + slot) * a.Hkv + kvh) * kD + piece * 8;
+      k[u] = *reinterpret_cast<const u32x4*>(a.k_new + at);
+      v[u] = *reinterpret_cast<const u32x4*>(a.v_new + at);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int slot = (c >> 4) + 8 * u, pos = col * kPage + slot;
+    int ke, ve;
+    const u32x2 kc = quantize_row(k[u], ke);
+    *reinterpret_cast<u32x2*>(&codes.v[slot][piece * 8]) = quantize_row(v[u], ve);
+    if (pos >= lo && pos < hi) {
+      *reinterpret_cast<u32x2*>(k_pages + slot * kD + piece * 8) = kc;
+      if (piece == 0) {
+        exponents[slot] = (int8_t)ke;
+        exponents[kPage + slot] = (int8_t)ve;
+      }
+    }
+  }
+  __syncthreads();
+  uint8_t vals[kPage];
+#pragma unroll
+  for (int slot = 0; slot < kPage; ++slot) vals[slot] = codes.v[slot][c];
+  uint8_t* vdst = v_pages + c * kPage;
+  if (hi - lo == kPage) {
+    u32x4 w;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      w[d] = (uint32_t)vals[4 * d] | (uint32_t)vals[4 * d + 1] << 8 | (uint32_t)vals[4 * d + 2] << 16 | (uint32_t)vals[4 * d + 3] << 24;
+    *reinterpret_cast<u32x4*>(vdst) = w;
+  } else {
+#pragma unroll
+    for (int slot = 0; slot < kPage; ++slot) {
+      const int pos = col * kPage + slot;
+      if (pos >= lo && pos < hi) vdst[slot] = vals[slot];
+    }
+  }
+  __syncthreads();                                        // (the next page's codes)
+}
+
+// One page, for the 128 threads of a workgroup.
+template <bool kFp8>
+__device__ __forceinline__ void write_prompt_page(const PrefillArgs& a, const int g, const int b, const int n, const int pos0,
+                                                  const int kvh, const int col) {
+  if constexpr (kFp8) {
+    __shared__ PromptCodes codes;
+    write_prompt_page_fp8(a, g, b, n, pos0, kvh, col, codes);
+  } else {
+    write_prompt_page_bf16(a, g, b, n, pos0, kvh, col);
+  }
+}
+
 // `cols` workgroups per (group, KV head): one for every column of the tables, or else for every so many-th of those that the chunk
 // touches, from the first on.
-template <bool kAll>
+template <bool kAll, bool kFp8>
 __global__ __launch_bounds__(kD) void kv_write_prompt_kernel(PrefillArgs a, int cols) {
   const int at = blockIdx.x % cols;
   const int gk = blockIdx.x / cols;
@@ -1005,10 +1086,10 @@ __global__ __launch_bounds__(kD) void kv_write_prompt_kernel(PrefillArgs a, int 
   if (n == 0) return;
   const int first = (int)((unsigned)pos0 / kPage), last = (int)((unsigned)(pos0 + n - 1) / kPage);
   if (kAll) {
-    if (at >= first && at <= last) write_prompt_page(a, g, a.q_start[g], n, pos0, kvh, at);
+    if (at >= first && at <= last) write_prompt_page<kFp8>(a, g, a.q_start[g], n, pos0, kvh, at);
   } else {
 #pragma unroll 1
-    for (int col = first + at; col <= last; col += cols) write_prompt_page(a, g, a.q_start[g], n, pos0, kvh, col);
+    for (int col = first + at; col <= last; col += cols) write_prompt_page<kFp8>(a, g, a.q_start[g], n, pos0, kvh, col);
   }
 }
 
@@ -1018,6 +1099,7 @@ __global__ __launch_bounds__(kD) void kv_write_prompt_kernel(PrefillArgs a, int 
 // the workgroup finds by itself: it looks at all of them (0.2 us of the call for 70, 0.7 for 210, 1.9 for 500), and so writes every group's pages
 // whatever the order of q_start.
 constexpr int kScatterGroups = 1024;
+template <bool kFp8>
 __global__ __launch_bounds__(kD) void kv_write_prompt_pages_kernel(PrefillArgs a) {
   extern __shared__ int4 chunk_of[];                     // [NG] first row, tokens, position, first column less its place
   __shared__ unsigned long long here[kScatterGroups / 64];
@@ -1039,7 +1121,7 @@ __global__ __launch_bounds__(kD) void kv_write_prompt_pages_kernel(PrefillArgs a
     if (blockIdx.x == 0 && c < 64 && flag && a.flags) atomicOr(a.flags, flag);
     for (unsigned long long m = __builtin_amdgcn_ballot_w64(mine); m != 0; m &= m - 1) {   // (one group, unless groups share rows)
       const int g = __builtin_ctzll(m);
-      write_prompt_page(a, g, __builtin_amdgcn_readlane(h.x, g), __builtin_amdgcn_readlane(h.y, g),
+      write_prompt_page<kFp8>(a, g, __builtin_amdgcn_readlane(h.x, g), __builtin_amdgcn_readlane(h.y, g),
                         __builtin_amdgcn_readlane(h.z, g), kvh, place + __builtin_amdgcn_readlane(h.w, g));
     }
     return;
@@ -1060,7 +1142,7 @@ __global__ __launch_bounds__(kD) void kv_write_prompt_pages_kernel(PrefillArgs a
     for (; m != 0; m &= m - 1) {
       const int g = 64 * w + __builtin_ctzll(m);
       const int4 h = chunk_of[g];
-      write_prompt_page(a, g, __builtin_amdgcn_readfirstlane(h.x), __builtin_amdgcn_readfirstlane(h.y),
+      write_prompt_page<kFp8>(a, g, __builtin_amdgcn_readfirstlane(h.x), __builtin_amdgcn_readfirstlane(h.y),
                         __builtin_amdgcn_readfirstlane(h.z), kvh, place + __builtin_amdgcn_readfirstlane(h.w));
     }
   }
@@ -1130,10 +1212,13 @@ hipError_t launch_kv_write_prompt(const PrefillArgs& a, hipStream_t st) {
   const bool few_empty = a.NG * all * a.Hkv <= 2048 || a.NG * all <= (places * a.Hkv >= 8192 ? 4 : 2) * places;
   long cols = few_empty ? all : std::min(all, 2 * mean + 2);
   const bool short_rounds = (all + cols - 1) / cols * (8 * 1100) <= places * a.Hkv * 3;   // ns; 16 KB at 5 TB/s a place and head
+  const bool fp8 = a.exponents_w != nullptr;
   if (few_empty || short_rounds || a.NG > kScatterGroups)
-    hipLaunchKernelGGL(cols == a.max_pp ? kv_write_prompt_kernel<true> : kv_write_prompt_kernel<false>, dim3((unsigned)(a.NG * a.Hkv * cols)), dim3(kD), 0, st, a, (int)cols);
+    hipLaunchKernelGGL(fp8 ? (cols == a.max_pp ? kv_write_prompt_kernel<true, true> : kv_write_prompt_kernel<false, true>)
+                           : (cols == a.max_pp ? kv_write_prompt_kernel<true, false> : kv_write_prompt_kernel<false, false>),
+                       dim3((unsigned)(a.NG * a.Hkv * cols)), dim3(kD), 0, st, a, (int)cols);
   else
-    hipLaunchKernelGGL(kv_write_prompt_pages_kernel, dim3((unsigned)(places * a.Hkv)), dim3(kD), a.NG <= 64 ? 0 : sizeof(int4) * a.NG, st, a);
+    hipLaunchKernelGGL(fp8 ? kv_write_prompt_pages_kernel<true> : kv_write_prompt_pages_kernel<false>, dim3((unsigned)(places * a.Hkv)), dim3(kD), a.NG <= 64 ? 0 : sizeof(int4) * a.NG, st, a);
   return hipGetLastError();
 }
 
