@@ -364,6 +364,11 @@ int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, con
  * src[i] stands for, all KV heads, keys and values, slots that no token owns included: for calls that take a bf16 cache, such
  * as marl_prefill_attn for a further chunk of a prompt.  src, dst: device int32 [n]; a dst must not appear twice in a call.  Pairs with
  * an id outside [0, num_pages) or [0, num_out_pages) are skipped and flagged (MARL_FLAG_BAD_PAGE in *flags, which may be NULL).
+ *
+ * marl_decode_attn_fp8: marl_decode_attn over such a cache: the same operation on the values that the codes stand for, the same shape,
+ * workspace (marl_workspace_bytes), work lists, flags and limits; q stays bf16.  A token's row whose exponent lies outside what the writing calls
+ * store ([-110, 120]) gives unspecified values, codes and exponents that no token owns are never read into a result.  The weights are
+ * rounded to bf16 before they multiply the values, as in marl_decode_attn; everything else is float32.
  */
 int marl_kv_append_fp8(const marl_attn_shape* shape, const void* k_new, const void* v_new,
                        void* k_pages, void* v_pages, int8_t* exponents, const int32_t* suffix_block_table,
@@ -374,6 +379,11 @@ int marl_kv_write_prompt_fp8(const marl_prefill_shape* shape, const void* k_new,
 int marl_kv_read_pages_fp8(int32_t num_kv_heads, int32_t num_pages, const void* k_codes, const void* v_codes,
                            const int8_t* exponents, int32_t num_out_pages, void* k_pages, void* v_pages,
                            const int32_t* src, const int32_t* dst, int32_t n, int32_t* flags, void* stream);
+int marl_decode_attn_fp8(const marl_attn_shape* shape, void* workspace, size_t workspace_bytes,
+                         const void* q, const void* k_pages, const void* v_pages, const int8_t* exponents,
+                         const int32_t* prefix_block_table, const int32_t* suffix_block_table,
+                         const int32_t* prefix_lens, const int32_t* suffix_lens,
+                         const int32_t* group_of_seq, float scale, void* out, void* stream);
 
 /*
  * Group-normalised advantages of GRPO (Shao et al. 2024; the paper trains every agent with

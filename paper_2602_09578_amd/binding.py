@@ -171,6 +171,8 @@ def load_library(build_if_missing: bool = True):
     lib.marl_pack_tensors.argtypes = [VP, I32, ctypes.c_int64, VP, VP]
     lib.marl_unpack_tensors.argtypes = [VP, I32, ctypes.c_int64, VP, VP]
     lib.marl_pack_plan.restype = lib.marl_pack_tensors.restype = lib.marl_unpack_tensors.restype = ctypes.c_int
+    lib.marl_decode_attn_fp8.argtypes = [PS, VP, SZ] + [VP] * 9 + [ctypes.c_float, VP, VP]
+    lib.marl_decode_attn_fp8.restype = ctypes.c_int
     lib.marl_kv_append_fp8.argtypes = [PS] + [VP] * 9
     lib.marl_kv_write_prompt_fp8.argtypes = [PP] + [VP] * 10
     lib.marl_kv_read_pages_fp8.argtypes = [I32, I32, VP, VP, VP, I32, VP, VP, VP, VP, I32, VP, VP]
@@ -267,12 +269,12 @@ def _require(t: Optional[torch.Tensor], name: str, dtype, shape=None):
 
 
 def _require_attn_operands(shape: AttnShape, q, k_pages, v_pages, prefix_block_table, suffix_block_table,
-                           prefix_lens, suffix_lens, group_of_seq, out):
+                           prefix_lens, suffix_lens, group_of_seq, out, pages_dtype=torch.bfloat16):
     NS, NG, Hq, Hkv = shape.num_seqs, shape.num_groups, shape.num_q_heads, shape.num_kv_heads
     bf, i32 = torch.bfloat16, torch.int32
     _require(q, "q", bf, (NS, Hq, 128))
-    _require(k_pages, "k_pages", bf, (shape.num_pages, Hkv, 16, 128))
-    _require(v_pages, "v_pages", bf, (shape.num_pages, Hkv, 128, 16))
+    _require(k_pages, "k_pages", pages_dtype, (shape.num_pages, Hkv, 16, 128))
+    _require(v_pages, "v_pages", pages_dtype, (shape.num_pages, Hkv, 128, 16))
     if shape.max_prefix_pages > 0:
         _require(prefix_block_table, "prefix_block_table", i32, (NG, shape.max_prefix_pages))
     if shape.max_suffix_pages > 0:
@@ -540,6 +542,21 @@ def _require_fp8_cache(num_pages, Hkv, k_pages, v_pages, exponents):
     _require(v_pages, "v_pages", FP8, (num_pages, Hkv, 128, 16))
     _require(exponents, "exponents", torch.int8, (num_pages, Hkv, 2, 16))
     _require_cuda(k_pages, v_pages, exponents)
+
+
+def marl_decode_attn_fp8(shape: AttnShape, workspace: torch.Tensor, q, k_pages, v_pages, exponents, prefix_block_table,
+                         suffix_block_table, prefix_lens, suffix_lens, group_of_seq, scale: float, out: torch.Tensor) -> torch.Tensor:
+    """marl_decode_attn over an 8-bit cache."""
+    _require_attn_operands(shape, q, k_pages, v_pages, prefix_block_table, suffix_block_table, prefix_lens,
+                           suffix_lens, group_of_seq, out, FP8)
+    _require_fp8_cache(shape.num_pages, shape.num_kv_heads, k_pages, v_pages, exponents)
+    _require_cuda(workspace, q, prefix_block_table, suffix_block_table, prefix_lens, suffix_lens, group_of_seq, out)
+    rc = load_library().marl_decode_attn_fp8(
+        ctypes.byref(shape), _ptr(workspace), workspace.numel(), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(exponents),
+        _ptr(prefix_block_table), _ptr(suffix_block_table), _ptr(prefix_lens), _ptr(suffix_lens),
+        _ptr(group_of_seq), float(scale), _ptr(out), _stream(out.device))
+    _check(rc, "marl_decode_attn_fp8")
+    return out
 
 
 def marl_kv_append_fp8(shape: AttnShape, k_new, v_new, k_pages, v_pages, exponents, suffix_block_table, suffix_lens,

@@ -132,7 +132,9 @@ struct StageTimer {
   }
 };
 
-int g_num_cus = 0, g_prefix_bpc = 0, g_prefix_wide_bpc = 0, g_suffix_bpc = 0, g_items_bpc = 0, g_items_wide_bpc = 0;
+int g_num_cus = 0;
+// workgroups per CU, by cache: [0] bf16, [1] 8 bit; by blocks of query rows: [1] wide
+int g_prefix_bpc[2][2], g_items_bpc[2][2], g_suffix_bpc[2];
 
 std::once_flag g_dev_once;
 hipError_t g_dev_err = hipSuccess;
@@ -145,11 +147,13 @@ void query_device() {
   g_dev_err = hipGetDeviceProperties(&p, dev);
   if (g_dev_err != hipSuccess) return;
   g_num_cus = p.multiProcessorCount;
-  g_prefix_bpc = marl::prefix_blocks_per_cu(false);
-  g_prefix_wide_bpc = marl::prefix_blocks_per_cu(true);
-  g_suffix_bpc = marl::suffix_blocks_per_cu();
-  g_items_bpc = marl::items_blocks_per_cu(false);
-  g_items_wide_bpc = marl::items_blocks_per_cu(true);
+  for (int fp8 = 0; fp8 < 2; ++fp8) {
+    for (int wide = 0; wide < 2; ++wide) {
+      g_prefix_bpc[fp8][wide] = marl::prefix_blocks_per_cu(wide, fp8);
+      g_items_bpc[fp8][wide] = marl::items_blocks_per_cu(wide, fp8);
+    }
+    g_suffix_bpc[fp8] = marl::suffix_blocks_per_cu(fp8);
+  }
 }
 
 // Points the workspace arrays of `a` into `ws` as the layout says.
@@ -253,22 +257,22 @@ int enqueue_decode_attn(marl::AttnArgs& a, bool default_chunks, hipStream_t st, 
   }
   if ((e = T.run(MARL_STAGE_PLAN, [&] { return marl::launch_plan(a, st); })) != hipSuccess)
     return hip_fail(e, "plan kernel");
-  const bool wide = a.qblock_rows == marl::kRowsPerQBlockWide;
+  const bool wide = a.qblock_rows == marl::kRowsPerQBlockWide, fp8 = a.exponents != nullptr;
   a.one_queue = (long)a.NS * a.Hkv <= marl::kOneQueueItems;
   if (a.one_queue) {
     if ((e = T.run(a.NG > 0 && a.max_pp > 0 && !can_have_long_items(a) ? MARL_STAGE_PREFIX : MARL_STAGE_SUFFIX,
-                   [&] { return marl::launch_items(a, g_num_cus * (wide ? g_items_wide_bpc : g_items_bpc), st); })) != hipSuccess)
+                   [&] { return marl::launch_items(a, g_num_cus * g_items_bpc[fp8][wide], st); })) != hipSuccess)
       return hip_fail(e, "items kernel");
     if ((e = T.run(MARL_STAGE_MERGE, [&] { return marl::launch_merge(a, st); })) != hipSuccess)
       return hip_fail(e, "merge kernel");
     return MARL_OK;
   }
   {  // always launched: its workgroups also process the short suffix items
-    if ((e = T.run(MARL_STAGE_PREFIX, [&] { return marl::launch_prefix(a, g_num_cus * (wide ? g_prefix_wide_bpc : g_prefix_bpc), st); })) != hipSuccess)
+    if ((e = T.run(MARL_STAGE_PREFIX, [&] { return marl::launch_prefix(a, g_num_cus * g_prefix_bpc[fp8][wide], st); })) != hipSuccess)
       return hip_fail(e, "prefix kernel");
   }
   if (can_have_long_items(a)) {
-    if ((e = T.run(MARL_STAGE_SUFFIX, [&] { return marl::launch_suffix(a, g_num_cus * g_suffix_bpc, st); })) != hipSuccess)
+    if ((e = T.run(MARL_STAGE_SUFFIX, [&] { return marl::launch_suffix(a, g_num_cus * g_suffix_bpc[fp8], st); })) != hipSuccess)
       return hip_fail(e, "suffix kernel");
   }
   if ((e = T.run(MARL_STAGE_MERGE, [&] { return marl::launch_merge(a, st); })) != hipSuccess)
@@ -363,6 +367,23 @@ int marl_decode_attn(const marl_attn_shape* shape, void* workspace, size_t works
                           suffix_lens, group_of_seq, scale, out);
   if (rc != MARL_OK) return rc;
   if (a.NS == 0) return MARL_OK;
+  return enqueue_decode_attn(a, default_chunks(shape), static_cast<hipStream_t>(stream), /*may_time=*/true);
+}
+
+int marl_decode_attn_fp8(const marl_attn_shape* shape, void* workspace, size_t workspace_bytes,
+                         const void* q, const void* k_pages, const void* v_pages, const int8_t* exponents,
+                         const int32_t* prefix_block_table, const int32_t* suffix_block_table,
+                         const int32_t* prefix_lens, const int32_t* suffix_lens,
+                         const int32_t* group_of_seq, float scale, void* out, void* stream) {
+  marl::AttnArgs a;
+  int rc = fill_args(shape, workspace, workspace_bytes, a);
+  if (rc != MARL_OK) return rc;
+  rc = take_attn_operands(a, q, k_pages, v_pages, prefix_block_table, suffix_block_table, prefix_lens,
+                          suffix_lens, group_of_seq, scale, out);
+  if (rc != MARL_OK) return rc;
+  if (a.NS == 0) return MARL_OK;
+  if (!exponents || !aligned16(exponents)) return MARL_INVALID_ARG;
+  a.exponents = exponents;
   return enqueue_decode_attn(a, default_chunks(shape), static_cast<hipStream_t>(stream), /*may_time=*/true);
 }
 

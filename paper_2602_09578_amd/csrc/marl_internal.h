@@ -54,6 +54,7 @@ struct AttnArgs {
   int32_t splits;        // small calls only
   int32_t one_queue;     // prefix and suffix items are taken by one kernel
   float scale;
+  const int8_t* exponents;   // of an 8-bit cache, whose codes k_pages and v_pages are then; null for a bf16 one
 };
 
 hipError_t launch_plan(const AttnArgs& a, hipStream_t st);
@@ -65,9 +66,9 @@ hipError_t launch_merge(const AttnArgs& a, hipStream_t st);
 int small_attn_splits(const AttnArgs& a);
 hipError_t launch_small_attn(const AttnArgs& a, hipStream_t st);
 hipError_t launch_merge_parts(const AttnArgs& a, hipStream_t st);
-int prefix_blocks_per_cu(bool wide);
-int items_blocks_per_cu(bool wide);
-int suffix_blocks_per_cu();
+int prefix_blocks_per_cu(bool wide, bool fp8);
+int items_blocks_per_cu(bool wide, bool fp8);
+int suffix_blocks_per_cu(bool fp8);
 
 struct KvAppendArgs {
   const uint16_t* k_new;

@@ -3,8 +3,8 @@
 Tolerances, from the formulas: a row's sum of squares is at most 8 + 5 roundings deep, of which the reciprocal root keeps half, and
 has 2 of its own; the weight, the angle and the two products add 5: 16 units of 2^-24 of the magnitudes that are added up, taken as
 24.  Backward the mean of g n adds as many (taken as 48), and a sum of dw is at most 4 + 2 + 4 + 64 additions deep for the rows of
-these tests (taken as 128).  A bf16 result is rounded once more: 2^-8 of its value (half of it by rounding to nearest, half for the
-case that the float32 value lies on the other side of a tie)."""
+these tests (taken as 128).  A bf16 result is rounded once more: to nearest of 8 significant
+bits, up to 2^-8 of its value."""
 import numpy as np
 import pytest
 import torch
