@@ -100,7 +100,9 @@ def _load_fast_calls(lib, build: bool):
         if sources is not None and getattr(m, "sources", None) != sources:
             raise ImportError(f"{FAST_PATH} was built from other sources")
         _bind_fast_calls(m, lib.marl_decode_attn, lib.marl_token_logprobs, lib.marl_kv_append, lib.marl_sample_tokens,
-                         lib.marl_sample_tokens_top_p, lib.marl_prefill_attn, lib.marl_kv_write_prompt)
+                         lib.marl_sample_tokens_top_p, lib.marl_prefill_attn, lib.marl_kv_write_prompt, lib.marl_decode_attn_fp8,
+                         lib.marl_kv_append_fp8, lib.marl_kv_write_prompt_fp8, lib.marl_kv_read_pages_fp8, lib.marl_qk_norm_rope,
+                         lib.marl_qk_norm_rope_backward)
         return m
     except (ImportError, OSError, RuntimeError, TypeError, AttributeError) as e:
         warnings.warn(f"calls take a few microseconds longer, without fast_calls: {e}", RuntimeWarning, stacklevel=3)
@@ -547,6 +549,13 @@ def _require_fp8_cache(num_pages, Hkv, k_pages, v_pages, exponents):
 def marl_decode_attn_fp8(shape: AttnShape, workspace: torch.Tensor, q, k_pages, v_pages, exponents, prefix_block_table,
                          suffix_block_table, prefix_lens, suffix_lens, group_of_seq, scale: float, out: torch.Tensor) -> torch.Tensor:
     """marl_decode_attn over an 8-bit cache."""
+    if _fast is not None:
+        rc = _fast.decode_attn_fp8(shape, workspace, q, k_pages, v_pages, exponents, prefix_block_table, suffix_block_table, prefix_lens,
+                                   suffix_lens, group_of_seq, scale, out)
+        if rc is not None:
+            if rc:
+                _check(rc, "marl_decode_attn_fp8")
+            return out
     _require_attn_operands(shape, q, k_pages, v_pages, prefix_block_table, suffix_block_table, prefix_lens,
                            suffix_lens, group_of_seq, out, FP8)
     _require_fp8_cache(shape.num_pages, shape.num_kv_heads, k_pages, v_pages, exponents)
@@ -562,6 +571,10 @@ def marl_decode_attn_fp8(shape: AttnShape, workspace: torch.Tensor, q, k_pages, 
 def marl_kv_append_fp8(shape: AttnShape, k_new, v_new, k_pages, v_pages, exponents, suffix_block_table, suffix_lens,
                        flags: Optional[torch.Tensor] = None):
     """marl_kv_append into an 8-bit cache."""
+    if _fast is not None:
+        rc = _fast.kv_append_fp8(shape, k_new, v_new, k_pages, v_pages, exponents, suffix_block_table, suffix_lens, flags)
+        if rc is not None:
+            return _check(rc, "marl_kv_append_fp8")
     NS, Hkv = shape.num_seqs, shape.num_kv_heads
     _require_cuda(k_new, v_new, suffix_block_table, suffix_lens, flags)
     _require_fp8_cache(shape.num_pages, Hkv, k_pages, v_pages, exponents)
@@ -578,6 +591,10 @@ def marl_kv_append_fp8(shape: AttnShape, k_new, v_new, k_pages, v_pages, exponen
 def marl_kv_write_prompt_fp8(shape: PrefillShape, k_new, v_new, k_pages, v_pages, exponents, prefix_block_table, q_start, q_pos0,
                              flags: Optional[torch.Tensor] = None):
     """marl_kv_write_prompt into an 8-bit cache."""
+    if _fast is not None:
+        rc = _fast.kv_write_prompt_fp8(shape, k_new, v_new, k_pages, v_pages, exponents, prefix_block_table, q_start, q_pos0, flags)
+        if rc is not None:
+            return _check(rc, "marl_kv_write_prompt_fp8")
     NT, NG, Hkv = shape.num_tokens, shape.num_groups, shape.num_kv_heads
     _require_cuda(k_new, v_new, prefix_block_table, q_start, q_pos0, flags)
     _require_fp8_cache(shape.num_pages, Hkv, k_pages, v_pages, exponents)
@@ -594,6 +611,10 @@ def marl_kv_write_prompt_fp8(shape: PrefillShape, k_new, v_new, k_pages, v_pages
 
 def marl_kv_read_pages_fp8(k_codes, v_codes, exponents, src, dst, k_pages, v_pages, flags: Optional[torch.Tensor] = None):
     """bf16 page dst[i] of k_pages / v_pages becomes what 8-bit page src[i] stands for."""
+    if _fast is not None:
+        rc = _fast.kv_read_pages_fp8(k_codes, v_codes, exponents, src, dst, k_pages, v_pages, flags)
+        if rc is not None:
+            return _check(rc, "marl_kv_read_pages_fp8")
     if k_codes.dim() != 4 or k_pages.dim() != 4:
         raise ValueError("k_codes, k_pages: expected [pages, Hkv, 16, 128]")
     pages, Hkv, out_pages, n = k_codes.shape[0], k_codes.shape[1], k_pages.shape[0], int(src.numel())
@@ -659,6 +680,12 @@ def marl_qk_norm_rope(q, k, q_weight, k_weight, cos_sin, positions, eps: float, 
                       flags: Optional[torch.Tensor] = None):
     """Norm of every head of q [tokens, Hq, D] and k [tokens, Hkv, D] with its weight, then rotation by position: see the header.
     cos_sin: float32 [max_positions, rotary_dim], or None for none.  q_out and k_out may be q and k themselves."""
+    if _fast is not None:
+        rc = _fast.qk_norm_rope(q, k, q_weight, k_weight, cos_sin, positions, eps, q_out, k_out, adjacent_pairs, flags)
+        if rc is not None:
+            if rc:
+                _check(rc, "marl_qk_norm_rope")
+            return q_out, k_out
     shape = _norm_rope_shape(q, k, q_weight, k_weight, cos_sin, positions, eps, adjacent_pairs, flags)
     shape.q_out_stride = _require_heads(q_out, "q_out", q.dtype, *q.shape)
     shape.k_out_stride = _require_heads(k_out, "k_out", q.dtype, *k.shape)
@@ -680,6 +707,13 @@ def marl_qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos_sin
                                workspace: torch.Tensor, adjacent_pairs: bool = False, flags: Optional[torch.Tensor] = None):
     """Gradients dq, dk (which may be dq_out and dk_out themselves) and dq_weight, dk_weight (float32, None: not wanted) of
     marl_qk_norm_rope from those of its results."""
+    if _fast is not None:
+        rc = _fast.qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos_sin, positions, eps, dq, dk, dq_weight, dk_weight,
+                                         workspace, adjacent_pairs, flags)
+        if rc is not None:
+            if rc:
+                _check(rc, "marl_qk_norm_rope_backward")
+            return dq, dk, dq_weight, dk_weight
     shape = _norm_rope_shape(q, k, q_weight, k_weight, cos_sin, positions, eps, adjacent_pairs, flags)
     shape.q_out_stride = _require_heads(dq_out, "dq_out", q.dtype, *q.shape)
     shape.k_out_stride = _require_heads(dk_out, "dk_out", q.dtype, *k.shape)
