@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWavesPerBlock = kThreads / 64;
-constexpr int kFinishThreads = 1024, kFinishColumns = 32;
+constexpr int kFinishThreads = 512, kFinishColumns = 16;
 
 // Eight channels of a head as they lie in memory.
 template <bool kF32>
@@ -30,6 +30,7 @@ template <>
 struct Piece<false> {
   u32x4 w;
   __device__ __forceinline__ void load(const char* p) { w = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ void load_once(const char* p) { w = ld_stream(p); }
   __device__ __forceinline__ void clear() { w = u32x4{0u, 0u, 0u, 0u}; }
   __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
   __device__ __forceinline__ Piece of_lane(int lane) const {
@@ -38,14 +39,18 @@ struct Piece<false> {
     for (int i = 0; i < 4; ++i) o.w[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * lane, (int)w[i]);
     return o;
   }
+  template <bool kPastCaches>
   static __device__ __forceinline__ void store(char* p, const float (&v)[8]) {
-    *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    const u32x4 o = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    if constexpr (kPastCaches) __builtin_nontemporal_store(o, reinterpret_cast<u32x4*>(p));
+    else *reinterpret_cast<u32x4*>(p) = o;
   }
 };
 template <>
 struct Piece<true> {
   f32x4 a, b;
   __device__ __forceinline__ void load(const char* p) { a = *reinterpret_cast<const f32x4*>(p); b = *reinterpret_cast<const f32x4*>(p + 16); }
+  __device__ __forceinline__ void load_once(const char* p) { load(p); }   // (two loads take turns in every line: through the caches)
   __device__ __forceinline__ void clear() { a = b = f32x4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ float at(int i) const { return i < 4 ? a[i] : b[i - 4]; }
   __device__ __forceinline__ Piece of_lane(int lane) const {
@@ -57,6 +62,7 @@ struct Piece<true> {
     }
     return o;
   }
+  template <bool>
   static __device__ __forceinline__ void store(char* p, const float (&v)[8]) {
     *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
     *reinterpret_cast<f32x4*>(p + 16) = f32x4{v[4], v[5], v[6], v[7]};
@@ -141,7 +147,7 @@ struct Steps {
   __device__ __forceinline__ explicit Steps(const NormRopeArgs& a) : q((a.Hq + kHeads - 1) / kHeads), all(q + (a.Hkv + kHeads - 1) / kHeads) {}
 };
 
-template <bool kF32, int D, bool kAdjacent, int kSteps>
+template <bool kF32, int D, bool kAdjacent, int kSteps, bool kPastCaches>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(NormRopeArgs a) {
   constexpr int kLanes = D / 8, kBytes = kF32 ? 4 : 2;
   const int lane = threadIdx.x & 63, sub = lane & (kLanes - 1), group = lane / kLanes;
@@ -163,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(NormRopeArgs a) 
     const int h = head_of(first + u, query, there);
     x[u].clear();
     if (there)
-      x[u].load(static_cast<const char*>(query ? a.q : a.k) + ((size_t)token * (query ? a.q_stride : a.k_stride) + (size_t)h * D + 8 * sub) * kBytes);
+      x[u].load_once(static_cast<const char*>(query ? a.q : a.k) + ((size_t)token * (query ? a.q_stride : a.k_stride) + (size_t)h * D + 8 * sub) * kBytes);
   }
   int flag = 0;
   const Turn<kAdjacent> turn(a, token, lane, sub, flag);
@@ -194,7 +200,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(NormRopeArgs a) 
 #pragma unroll
     for (int i = 0; i < 8; ++i) z[i] = r * __builtin_fmaf(x[u].at(i), A[i], (kAdjacent ? x[u].at(i ^ 1) : xp.at(i)) * B[i]);
     if (there)
-      Piece<kF32>::store(static_cast<char*>(query ? a.q_out : a.k_out) +
+      Piece<kF32>::template store<kPastCaches>(static_cast<char*>(query ? a.q_out : a.k_out) +
                          ((size_t)token * (query ? a.q_out_stride : a.k_out_stride) + (size_t)h * D + 8 * sub) * kBytes, z);
   }
   if (flag && a.flags) atomicOr(a.flags, flag);
@@ -203,7 +209,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(NormRopeArgs a) 
 // Backward.  The waves stay and take every so many-th unit, so that dw of the heads that a lane sees stays in its registers; a
 // workgroup adds its waves' sums through LDS and leaves one row of 2 D numbers, which the second kernel adds in their order
 // (no atomics: the same bits in every run).
-template <bool kF32, int D, bool kAdjacent, int kSteps>
+template <bool kF32, int D, bool kAdjacent, int kSteps, bool kPastCaches>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_backward_kernel(NormRopeArgs a) {
   constexpr int kLanes = D / 8, kBytes = kF32 ? 4 : 2;
   __shared__ float sums[kWavesPerBlock][2][D];
@@ -229,8 +235,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_backward_kernel(NormRop
       dz[u].clear();
       if (there) {
         const size_t at = (size_t)h * D + 8 * sub;
-        x[u].load(static_cast<const char*>(query ? a.q : a.k) + ((size_t)token * (query ? a.q_stride : a.k_stride) + at) * kBytes);
-        dz[u].load(static_cast<const char*>(query ? a.dq_out : a.dk_out) + ((size_t)token * (query ? a.q_out_stride : a.k_out_stride) + at) * kBytes);
+        x[u].load_once(static_cast<const char*>(query ? a.q : a.k) + ((size_t)token * (query ? a.q_stride : a.k_stride) + at) * kBytes);
+        dz[u].load_once(static_cast<const char*>(query ? a.dq_out : a.dk_out) + ((size_t)token * (query ? a.q_out_stride : a.k_out_stride) + at) * kBytes);
       }
     }
     const Turn<kAdjacent> turn(a, token, lane, sub, flag);
@@ -263,7 +269,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_backward_kernel(NormRop
         for (int i = 0; i < 8; ++i) dwk[i] = __builtin_fmaf(dy[i], x[u].at(i) * r, dwk[i]);
       }
       if (there)
-        Piece<kF32>::store(static_cast<char*>(query ? a.dq : a.dk) +
+        Piece<kF32>::template store<kPastCaches>(static_cast<char*>(query ? a.dq : a.dk) +
                            ((size_t)token * (query ? a.dq_stride : a.dk_stride) + (size_t)h * D + 8 * sub) * kBytes, dx);
     }
   }
@@ -289,41 +295,54 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_backward_kernel(NormRop
   }
 }
 
-// dw of the queries (columns 0 .. D - 1) and of the keys: sums of the workgroups' rows, 32 columns a workgroup.
+// dw of the queries (columns 0 .. D - 1) and of the keys: sums of the workgroups' rows, 16 columns a workgroup.  A thread requests
+// eight rows before it adds the first (one after the other: 12 us for 1024 rows).
 __global__ __launch_bounds__(kFinishThreads) void qk_norm_weight_grad_kernel(NormRopeArgs a, int rows, int D) {
-  constexpr int kSlices = kFinishThreads / kFinishColumns;
+  constexpr int kSlices = kFinishThreads / kFinishColumns, kAtOnce = 8;
   __shared__ float part[kSlices][kFinishColumns];
-  const int column = blockIdx.x * kFinishColumns + threadIdx.x % kFinishColumns, slice = threadIdx.x / kFinishColumns;
-  float v = 0.f;
-  for (int r = slice; r < rows; r += kSlices) v += a.partials[(size_t)r * (2 * D) + column];
-  part[slice][threadIdx.x % kFinishColumns] = v;
+  const int c = threadIdx.x % kFinishColumns, column = blockIdx.x * kFinishColumns + c, slice = threadIdx.x / kFinishColumns;
+  const float* from = a.partials + column;
+  float sum[kAtOnce] = {};
+  for (int r = slice; r < rows; r += kSlices * kAtOnce) {
+    float v[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) v[u] = r + u * kSlices < rows ? from[(size_t)(r + u * kSlices) * (2 * D)] : 0.f;
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) sum[u] += v[u];
+  }
+  part[slice][c] = ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
   __syncthreads();
   if (slice != 0) return;
-  v = 0.f;
+  float v = 0.f;
 #pragma unroll
-  for (int k = 0; k < kSlices; ++k) v += part[k][threadIdx.x];
+  for (int k = 0; k < kSlices; ++k) v += part[k][c];
   float* out = column < D ? a.dq_weight : a.dk_weight;
   if (out) out[column < D ? column : column - D] = v;
 }
 
-// A wave's steps at once.  Many, where there are waves enough for the GPU's 256 CUs: the table row, the weights and the launch
-// of a wave are shared by more heads; few, where a call is small and waits for its loads.
-constexpr int kManySteps = 8, kManyStepsF32 = 4, kFewSteps = 2, kBackwardSteps = 4, kBackwardStepsF32 = 2;
-constexpr long kEnoughUnits = 4096;
+// A wave's steps at once: four, where there are waves enough for the GPU's 256 CUs (eight: 189 instead of 182 us for 65543 tokens of 28
+// + 4 heads of 128, two 169 instead of 161 for the gradient of 32771); few, where a call is small and waits for its loads.
+constexpr int kManySteps = 4, kFewSteps = 2, kBackwardSteps = 4, kBackwardStepsF32 = 2;
+constexpr long kEnoughUnits = 8192;
+// Results that the caches of the XCDs (4 MB each) cannot hold until somebody reads them are stored past them: 194 -> 187 us for the
+// 65543 tokens, 170 -> 161 for the gradient of 32771.
+constexpr long kCacheBytes = 32l << 20;
+bool past_caches(const NormRopeArgs& a) { return (long)a.T * (a.Hq + a.Hkv) * a.D * (a.f32 ? 4 : 2) > kCacheBytes; }
 
 int steps_of(const NormRopeArgs& a) { const int heads = 512 / a.D; return (a.Hq + heads - 1) / heads + (a.Hkv + heads - 1) / heads; }
 
 template <bool kF32, int D, bool kAdjacent>
 hipError_t launch_forward(NormRopeArgs a, hipStream_t st) {
-  constexpr int kMany = kF32 ? kManyStepsF32 : kManySteps;
   const long all = steps_of(a);
-  const bool many = (long)a.T * ((all + kMany - 1) / kMany) >= kEnoughUnits;
-  const int steps = many ? kMany : kFewSteps;
+  const bool many = (long)a.T * ((all + kManySteps - 1) / kManySteps) >= kEnoughUnits;
+  const int steps = many ? kManySteps : kFewSteps;
   a.units_per_token = (int)((all + steps - 1) / steps);
   a.units = (int)((long)a.T * a.units_per_token);
   const dim3 grid((unsigned)((a.units + kWavesPerBlock - 1) / kWavesPerBlock));
-  if (many) hipLaunchKernelGGL((qk_norm_rope_kernel<kF32, D, kAdjacent, kMany>), grid, dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((qk_norm_rope_kernel<kF32, D, kAdjacent, kFewSteps>), grid, dim3(kThreads), 0, st, a);
+  // (few steps, 8192 units of them or fewer: at most 16 MB)
+  if (many && past_caches(a)) hipLaunchKernelGGL((qk_norm_rope_kernel<kF32, D, kAdjacent, kManySteps, true>), grid, dim3(kThreads), 0, st, a);
+  else if (many) hipLaunchKernelGGL((qk_norm_rope_kernel<kF32, D, kAdjacent, kManySteps, false>), grid, dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((qk_norm_rope_kernel<kF32, D, kAdjacent, kFewSteps, false>), grid, dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 
@@ -334,7 +353,8 @@ hipError_t launch_backward(NormRopeArgs a, hipStream_t st) {
   a.units = (int)((long)a.T * a.units_per_token);
   const int blocks = std::min((a.units + kWavesPerBlock - 1) / kWavesPerBlock, kNormRopeMaxBlocks);
   if (blocks > 0) {
-    hipLaunchKernelGGL((qk_norm_rope_backward_kernel<kF32, D, kAdjacent, kSteps>), dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
+    if (past_caches(a)) hipLaunchKernelGGL((qk_norm_rope_backward_kernel<kF32, D, kAdjacent, kSteps, true>), dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((qk_norm_rope_backward_kernel<kF32, D, kAdjacent, kSteps, false>), dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
