@@ -132,9 +132,8 @@ struct StageTimer {
   }
 };
 
-int g_num_cus = 0;
-// workgroups per CU, by cache: [0] bf16, [1] 8 bit; by blocks of query rows: [1] wide
-int g_prefix_bpc[2][2], g_items_bpc[2][2], g_suffix_bpc[2];
+int g_num_cus = 0, g_prefix_bpc = 0, g_prefix_wide_bpc = 0, g_suffix_bpc = 0, g_items_bpc = 0, g_items_wide_bpc = 0;
+int g_items_fp8_bpc = 0, g_items_fp8_wide_bpc = 0;
 
 std::once_flag g_dev_once;
 hipError_t g_dev_err = hipSuccess;
@@ -147,13 +146,13 @@ void query_device() {
   g_dev_err = hipGetDeviceProperties(&p, dev);
   if (g_dev_err != hipSuccess) return;
   g_num_cus = p.multiProcessorCount;
-  for (int fp8 = 0; fp8 < 2; ++fp8) {
-    for (int wide = 0; wide < 2; ++wide) {
-      g_prefix_bpc[fp8][wide] = marl::prefix_blocks_per_cu(wide, fp8);
-      g_items_bpc[fp8][wide] = marl::items_blocks_per_cu(wide, fp8);
-    }
-    g_suffix_bpc[fp8] = marl::suffix_blocks_per_cu(fp8);
-  }
+  g_prefix_bpc = marl::prefix_blocks_per_cu(false);
+  g_prefix_wide_bpc = marl::prefix_blocks_per_cu(true);
+  g_suffix_bpc = marl::suffix_blocks_per_cu();
+  g_items_bpc = marl::items_blocks_per_cu(false);
+  g_items_wide_bpc = marl::items_blocks_per_cu(true);
+  g_items_fp8_bpc = marl::items_fp8_blocks_per_cu(false);
+  g_items_fp8_wide_bpc = marl::items_fp8_blocks_per_cu(true);
 }
 
 // Points the workspace arrays of `a` into `ws` as the layout says.
@@ -249,7 +248,7 @@ int enqueue_decode_attn(marl::AttnArgs& a, bool default_chunks, hipStream_t st, 
   StageTimer T(st, timed);
   hipError_t e;
   if (default_chunks && (a.splits = marl::small_attn_splits(a)) > 0) {
-    if ((e = T.run(MARL_STAGE_PREFIX, [&] { return marl::launch_small_attn(a, st); })) != hipSuccess)
+    if ((e = T.run(MARL_STAGE_PREFIX, [&] { return a.exponents ? marl::launch_small_attn_fp8(a, st) : marl::launch_small_attn(a, st); })) != hipSuccess)
       return hip_fail(e, "small attention kernel");
     if (a.splits > 1 && (e = T.run(MARL_STAGE_MERGE, [&] { return marl::launch_merge_parts(a, st); })) != hipSuccess)
       return hip_fail(e, "merge kernel");
@@ -257,22 +256,29 @@ int enqueue_decode_attn(marl::AttnArgs& a, bool default_chunks, hipStream_t st, 
   }
   if ((e = T.run(MARL_STAGE_PLAN, [&] { return marl::launch_plan(a, st); })) != hipSuccess)
     return hip_fail(e, "plan kernel");
-  const bool wide = a.qblock_rows == marl::kRowsPerQBlockWide, fp8 = a.exponents != nullptr;
+  const bool wide = a.qblock_rows == marl::kRowsPerQBlockWide;
+  if (a.exponents) {   // an 8-bit cache: all items in one kernel, whatever their number
+    if ((e = T.run(MARL_STAGE_SUFFIX, [&] { return marl::launch_items_fp8(a, g_num_cus * (wide ? g_items_fp8_wide_bpc : g_items_fp8_bpc), st); })) != hipSuccess)
+      return hip_fail(e, "8-bit items kernel");
+    if ((e = T.run(MARL_STAGE_MERGE, [&] { return marl::launch_merge_fp8(a, st); })) != hipSuccess)
+      return hip_fail(e, "8-bit merge kernel");
+    return MARL_OK;
+  }
   a.one_queue = (long)a.NS * a.Hkv <= marl::kOneQueueItems;
   if (a.one_queue) {
     if ((e = T.run(a.NG > 0 && a.max_pp > 0 && !can_have_long_items(a) ? MARL_STAGE_PREFIX : MARL_STAGE_SUFFIX,
-                   [&] { return marl::launch_items(a, g_num_cus * g_items_bpc[fp8][wide], st); })) != hipSuccess)
+                   [&] { return marl::launch_items(a, g_num_cus * (wide ? g_items_wide_bpc : g_items_bpc), st); })) != hipSuccess)
       return hip_fail(e, "items kernel");
     if ((e = T.run(MARL_STAGE_MERGE, [&] { return marl::launch_merge(a, st); })) != hipSuccess)
       return hip_fail(e, "merge kernel");
     return MARL_OK;
   }
   {  // always launched: its workgroups also process the short suffix items
-    if ((e = T.run(MARL_STAGE_PREFIX, [&] { return marl::launch_prefix(a, g_num_cus * g_prefix_bpc[fp8][wide], st); })) != hipSuccess)
+    if ((e = T.run(MARL_STAGE_PREFIX, [&] { return marl::launch_prefix(a, g_num_cus * (wide ? g_prefix_wide_bpc : g_prefix_bpc), st); })) != hipSuccess)
       return hip_fail(e, "prefix kernel");
   }
   if (can_have_long_items(a)) {
-    if ((e = T.run(MARL_STAGE_SUFFIX, [&] { return marl::launch_suffix(a, g_num_cus * g_suffix_bpc[fp8], st); })) != hipSuccess)
+    if ((e = T.run(MARL_STAGE_SUFFIX, [&] { return marl::launch_suffix(a, g_num_cus * g_suffix_bpc, st); })) != hipSuccess)
       return hip_fail(e, "suffix kernel");
   }
   if ((e = T.run(MARL_STAGE_MERGE, [&] { return marl::launch_merge(a, st); })) != hipSuccess)

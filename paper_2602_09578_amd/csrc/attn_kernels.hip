@@ -28,7 +28,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "kv_step.h"
+#include "attn_shared.h"
 #include "marl_internal.h"
 #include "wave_ops.h"
 
@@ -36,12 +36,10 @@ namespace marl {
 namespace {
 
 constexpr int kWaves = kAttnThreads / 64;
-constexpr int kMaximaAtOnce = 8;   // of partials that are about to be added
 
 // LDS per workgroup for the cross-wave combine: (max, sum) and the row index of every q-row, and
 // every wave's accumulators in row-major order (a row is 128 floats, padded to 132 so that the
 // 16 rows a wave instruction writes start in different banks).
-constexpr int kAccRowFloats = kD + 4;
 template <int MT>
 struct ItemLds {
   float m[kWaves][MT * 16];
@@ -62,7 +60,7 @@ struct ItemLds {
 //   earlier kernel has completed: they are merged with the item's own result (the merge
 //   kernel's formula and order: prefix slots first) and the final output rows are written
 //   instead of a partial.
-template <int MT, int NW, bool kFp8>
+template <int MT, int NW>
 __device__ __forceinline__ void process_item(const AttnArgs& a, const int32_t* __restrict__ table_row,
                                              const int tok_begin, const int tok_end, const int kvh,
                                              const int (&row_index)[MT], const int slot,
@@ -75,9 +73,8 @@ __device__ __forceinline__ void process_item(const AttnArgs& a, const int32_t* _
   const float sc = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1e-30f);
   const uint32_t sign_flip = a.scale < 0.f ? 0x80008000u : 0u;
   const int nslot = a.NCp + a.NCs;
-  typedef KvStep<kFp8> Step;
 
-  // Q^T operand: lane (i, j) holds the channels of q-row i that it holds of the keys (8*(4*kk + j) .. +8 of a bf16 cache)
+  // Q^T operand: lane (i, j) holds channels 8*(4*kk + j) .. +8 of q-row i
   u32x4 qreg[MT][4];
   auto ready_q = [&] {
 #pragma unroll
@@ -92,11 +89,11 @@ __device__ __forceinline__ void process_item(const AttnArgs& a, const int32_t* _
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
       if constexpr (NW == 1) {   // without a branch, and used only once the first keys and values are requested too
-        qreg[qt][kk] = *reinterpret_cast<const u32x4*>(a.q + (size_t)max(row_index[qt], 0) * kD + Step::channel(kk, j));
+        qreg[qt][kk] = *reinterpret_cast<const u32x4*>(a.q + (size_t)max(row_index[qt], 0) * kD + (4 * kk + j) * 8);
       } else {
         u32x4 v = {0u, 0u, 0u, 0u};
         if (row_index[qt] >= 0) {
-          v = *reinterpret_cast<const u32x4*>(a.q + (size_t)row_index[qt] * kD + Step::channel(kk, j));
+          v = *reinterpret_cast<const u32x4*>(a.q + (size_t)row_index[qt] * kD + (4 * kk + j) * 8);
           v ^= sign_flip;
         }
         qreg[qt][kk] = v;
@@ -114,21 +111,32 @@ __device__ __forceinline__ void process_item(const AttnArgs& a, const int32_t* _
     for (int ct = 0; ct < 8; ++ct) acc[qt][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  KvRegisters<kFp8, true> kv(a, kvh, i, j);
+  const size_t page_bytes = (size_t)a.Hkv * (kPage * kD * 2);
+  const char* kbase = reinterpret_cast<const char*>(a.k_pages) + (size_t)kvh * (kPage * kD * 2) +
+                      ((8 * ((i >> 2) & 1) + (i & 3)) * (kD * 2) + j * 16);
+  const char* vbase = reinterpret_cast<const char*>(a.v_pages) + (size_t)kvh * (kPage * kD * 2) +
+                      (i * (kPage * 2) + (j & 1) * 16);
 
-  // Page ids of the step that starts at token t (wave-uniform, scalar loads).
-  auto load_pages = [&](int t, int (&p)[Step::kPages]) {
-    p[0] = ld_uniform(table_row + (t >> 4));
-    if constexpr (kFp8) {
-      const int last = (tok_end - 1) >> 4;
+  // Page ids of the 32-token step that starts at token t (wave-uniform, scalar loads).
+  auto load_pages = [&](int t, int& p0, int& p1) {
+    p0 = ld_uniform(table_row + (t >> 4));
+    p1 = (t + kPage < tok_end) ? ld_uniform(table_row + (t >> 4) + 1) : p0;
+    if ((unsigned)p0 >= (unsigned)a.num_pages) { p0 = 0; bad_page = 1; }
+    if ((unsigned)p1 >= (unsigned)a.num_pages) { p1 = 0; bad_page = 1; }
+  };
+  u32x4 kr[2][4], vr[8];
+  auto issue_k = [&](int p0, int p1) {
+    const char* kp = kbase + (size_t)(i < 8 ? p0 : p1) * page_bytes;
 #pragma unroll
-      for (int u = 1; u < Step::kPages; ++u) p[u] = ld_uniform(table_row + min((t >> 4) + u, last));
-    } else {
-      p[1] = (t + kPage < tok_end) ? ld_uniform(table_row + (t >> 4) + 1) : p[0];
-    }
+    for (int T = 0; T < 2; ++T)
 #pragma unroll
-    for (int u = 0; u < Step::kPages; ++u)
-      if ((unsigned)p[u] >= (unsigned)a.num_pages) { p[u] = 0; bad_page = 1; }
+      for (int kk = 0; kk < 4; ++kk)
+        kr[T][kk] = ld_stream_k(kp + T * (4 * kD * 2) + kk * 64);
+  };
+  auto issue_v = [&](int p0, int p1) {
+    const char* vp = vbase + (size_t)(j < 2 ? p0 : p1) * page_bytes;
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) vr[ct] = ld_stream(vp + ct * (16 * kPage * 2));
   };
 
   // Software pipeline: the K registers are refilled for the next step as soon as the score
@@ -136,10 +144,10 @@ __device__ __forceinline__ void process_item(const AttnArgs& a, const int32_t* _
   // fetched one step ahead.  So a wave keeps 16 KB of loads in flight while it computes.
   // The last step of a wave is peeled (no refill; it alone can be ragged) so that the loop
   // body has no conditional loads and every wait leaves the younger 8 loads in flight.
-  constexpr int stride = NW * Step::kTok;
-  int t0 = tok_begin + wave * Step::kTok;
+  constexpr int stride = NW * kBlockTok;
+  int t0 = tok_begin + wave * kBlockTok;
   int tn = t0 + stride;
-  int next[Step::kPages] = {};
+  int n0 = 0, n1 = 0;
 
   // a one-wave item's first prefix partial: max and sum with the queries, values in the place of the last keys
   float2 ml0 = make_float2(-INFINITY, 0.f);
@@ -151,12 +159,16 @@ __device__ __forceinline__ void process_item(const AttnArgs& a, const int32_t* _
 
   auto step = [&](auto has_next_tag) {
     constexpr bool kHasNext = decltype(has_next_tag)::value;
-    f32x4 s[MT][Step::kTiles];
+    f32x4 s[MT][2];
 #pragma unroll
     for (int qt = 0; qt < MT; ++qt)
 #pragma unroll
-      for (int T = 0; T < Step::kTiles; ++T) s[qt][T] = kv.scores(T, qreg[qt]);
-    if constexpr (kHasNext) kv.issue_k(next);
+      for (int T = 0; T < 2; ++T) {
+        s[qt][T] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) s[qt][T] = mfma_16x16x32(kr[T][kk], qreg[qt][kk], s[qt][T]);
+      }
+    if constexpr (kHasNext) issue_k(n0, n1);
 
     if constexpr (!kHasNext) {
       if constexpr (NW == 1) {
@@ -165,80 +177,68 @@ __device__ __forceinline__ void process_item(const AttnArgs& a, const int32_t* _
           for (int ct = 0; ct < 8; ++ct) o0[ct] = *reinterpret_cast<const f32x4*>(o0_src + 16 * ct);
         }
       }
-      if (t0 + Step::kTok > tok_end) {   // wave-uniform: the ragged end of a chunk
+      if (t0 + kBlockTok > tok_end) {   // wave-uniform: the ragged end of a chunk
         // tokens past the end: score -inf (weight 0), and zero their value slots, which may
         // hold anything (NaN included)
 #pragma unroll
         for (int qt = 0; qt < MT; ++qt)
 #pragma unroll
-          for (int T = 0; T < Step::kTiles; ++T)
+          for (int T = 0; T < 2; ++T)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (t0 + Step::kLaneTok * j + 4 * T + e >= tok_end) s[qt][T][e] = -INFINITY;
+              if (t0 + 8 * j + 4 * T + e >= tok_end) s[qt][T][e] = -INFINITY;
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          const uint32_t mask = value_mask<kFp8>(t0 + Step::kLaneTok * j, tok_end, d);
+          const int tok = t0 + 8 * j + 2 * d;
+          const uint32_t mask = (tok < tok_end ? 0x0000ffffu : 0u) | (tok + 1 < tok_end ? 0xffff0000u : 0u);
 #pragma unroll
-          for (int ct = 0; ct < 8; ++ct) kv.vr[ct][d] &= mask;
+          for (int ct = 0; ct < 8; ++ct) vr[ct][d] &= mask;
         }
       }
     }
 
-    u32x4 pb[MT][Step::kHalves];
+    u32x4 pb[MT];
 #pragma unroll
     for (int qt = 0; qt < MT; ++qt) {
-      float mx[Step::kHalves];
-#pragma unroll
-      for (int h = 0; h < Step::kHalves; ++h) {
-        const f32x4 s0 = s[qt][2 * h], s1 = s[qt][2 * h + 1];
-        mx[h] = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])),
-                      fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-      }
-      if constexpr (kFp8) mx[0] = fmaxf(mx[0], mx[1]);
-      mx[0] = rows_allreduce_max(mx[0]);
-      const float m_new = fmaxf(m_run[qt], mx[0] * sc);
+      const f32x4 s0 = s[qt][0], s1 = s[qt][1];
+      float mx = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])),
+                       fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+      mx = rows_allreduce_max(mx);
+      const float m_new = fmaxf(m_run[qt], mx * sc);
       const float alpha = __builtin_amdgcn_exp2f(m_run[qt] - m_new);
-      float p[8 * Step::kHalves], psum[Step::kHalves];
+      float p[8];
 #pragma unroll
-      for (int h = 0; h < Step::kHalves; ++h) {
-        float* ph = p + 8 * h;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          ph[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][2 * h][e], sc, -m_new));
-          ph[4 + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][2 * h + 1][e], sc, -m_new));
-        }
-        psum[h] = ((ph[0] + ph[1]) + (ph[2] + ph[3])) + ((ph[4] + ph[5]) + (ph[6] + ph[7]));
+      for (int e = 0; e < 4; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s0[e], sc, -m_new));
+        p[4 + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s1[e], sc, -m_new));
       }
-      if constexpr (kFp8) psum[0] += psum[1];
+      const float psum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       if (__builtin_amdgcn_ballot_w64(m_new > m_run[qt]) != 0) {   // wave-uniform
 #pragma unroll
         for (int ct = 0; ct < 8; ++ct) acc[qt][ct] *= alpha;
       }
-      l_run[qt] = l_run[qt] * alpha + psum[0];
+      l_run[qt] = l_run[qt] * alpha + psum;
       m_run[qt] = m_new;
-#pragma unroll
-      for (int h = 0; h < Step::kHalves; ++h) pb[qt][h] = weight_operand<kFp8>(p + 8 * h, kFp8 ? kv.vx[2 * h] : 0u, kFp8 ? kv.vx[2 * h + 1] : 0u);
+      pb[qt] = u32x4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
     }
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
-      for (int h = 0; h < Step::kHalves; ++h)
-#pragma unroll
-        for (int qt = 0; qt < MT; ++qt) acc[qt][ct] = mfma_16x16x32(value_operand<kFp8>(kv.vr[ct], h), pb[qt][h], acc[qt][ct]);
+      for (int qt = 0; qt < MT; ++qt) acc[qt][ct] = mfma_16x16x32(vr[ct], pb[qt], acc[qt][ct]);
 
     if constexpr (kHasNext) {
-      kv.issue_v(next);
+      issue_v(n0, n1);
       t0 = tn;
       tn += stride;
-      if (tn < tok_end) load_pages(tn, next);
+      if (tn < tok_end) load_pages(tn, n0, n1);
     }
   };
 
   if (t0 < tok_end) {
-    load_pages(t0, next);
-    kv.issue_k(next);
-    kv.issue_v(next);
-    if (tn < tok_end) load_pages(tn, next);
+    load_pages(t0, n0, n1);
+    issue_k(n0, n1);
+    issue_v(n0, n1);
+    if (tn < tok_end) load_pages(tn, n0, n1);
     if constexpr (NW == 1) ready_q();
     while (tn < tok_end) step(std::true_type{});
     step(std::false_type{});
@@ -413,8 +413,9 @@ __device__ __forceinline__ void process_item(const AttnArgs& a, const int32_t* _
 #define MARL_SUFFIX_WAVES 4
 #endif
 constexpr int kSuffixWaves = MARL_SUFFIX_WAVES;   // waves that share one long item (= workgroup size / 64)
-template <bool kFp8>
-__device__ __forceinline__ void suffix_kernel_body(const AttnArgs& a) {
+__global__ __launch_bounds__(kSuffixWaves * 64)
+__attribute__((amdgpu_waves_per_eu(MARL_SUFFIX_WAVES_PER_EU, MARL_SUFFIX_WAVES_PER_EU)))
+void suffix_kernel(AttnArgs a) {
   __shared__ ItemLds<1> lds;
   __shared__ int next_item;
   const int n_work = a.counters[MARL_CTR_NUM_LONG_SUFFIX_ITEMS] * a.Hkv;
@@ -438,17 +439,11 @@ __device__ __forceinline__ void suffix_kernel_body(const AttnArgs& a) {
     const int row_index[1] = {i < a.R ? s * a.Hq + kvh * a.R + i : -1};
     // a sequence whose own tokens are this one item: the output rows are finished here
     const int chunks = ld_uniform(a.seq_chunks + s);
-    process_item<1, kSuffixWaves, kFp8>(a, a.suffix_table + (size_t)s * a.max_sp, it.y, it.z, kvh, row_index,
-                                        a.NCp + it.y / a.Cs, lds, bad_page, (chunks >> 16) == 1, chunks & 0xffff);
+    process_item<1, kSuffixWaves>(a, a.suffix_table + (size_t)s * a.max_sp, it.y, it.z, kvh, row_index,
+                                  a.NCp + it.y / a.Cs, lds, bad_page, (chunks >> 16) == 1, chunks & 0xffff);
   }
   if (bad_page) atomicOr(&a.counters[MARL_CTR_FLAGS], MARL_FLAG_BAD_PAGE);
 }
-__global__ __launch_bounds__(kSuffixWaves * 64)
-__attribute__((amdgpu_waves_per_eu(MARL_SUFFIX_WAVES_PER_EU, MARL_SUFFIX_WAVES_PER_EU)))
-void suffix_kernel(AttnArgs a) { suffix_kernel_body<false>(a); }
-__global__ __launch_bounds__(kSuffixWaves * 64)
-__attribute__((amdgpu_waves_per_eu(2, 2)))
-void suffix_fp8_kernel(AttnArgs a) { suffix_kernel_body<true>(a); }
 
 // Short suffix items: wave w of the grid takes the entries n_long + w, n_long + w + W, ...
 // (W = waves in the grid) with no LDS, no barrier and no atomic: the entries are sorted by
@@ -463,7 +458,7 @@ void suffix_fp8_kernel(AttnArgs a) { suffix_kernel_body<true>(a); }
 // while the last step is computed, in the last keys' registers (with the queries it had spilled): 8192 sequences of 40 tokens
 // behind 256, 28 / 4 heads, 228 -> 220 us (1.0 GB); of up to 60 behind 64: 200 -> 193; 64 x 32 of up to 64 behind 4096: 50.4 ->
 // 47.  (Records and page ids an item ahead, in three workgroups per CU that stay: the same to 1 us.)
-template <bool kFinish, bool kFp8>
+template <bool kFinish>
 __device__ __forceinline__ void short_suffix_items(const AttnArgs& a, int& bad_page) {
   const int n_long = a.counters[MARL_CTR_NUM_LONG_SUFFIX_ITEMS] * a.Hkv;
   const int n_work = a.counters[MARL_CTR_NUM_SUFFIX_ITEMS] * a.Hkv;
@@ -482,8 +477,8 @@ __device__ __forceinline__ void short_suffix_items(const AttnArgs& a, int& bad_p
     if (((chunks >> 16) == 1) == kFinish) {
       const int row_index[1] = {i < a.R ? s * a.Hq + kvh * a.R + i : -1};
       ItemLds<1>* no_lds = nullptr;   // the one-wave path never touches it
-      process_item<1, 1, kFp8>(a, a.suffix_table + (size_t)s * a.max_sp, rec.y, rec.z, kvh, row_index,
-                               a.NCp + rec.y / a.Cs, *no_lds, bad_page, kFinish, chunks & 0xffff);
+      process_item<1, 1>(a, a.suffix_table + (size_t)s * a.max_sp, rec.y, rec.z, kvh, row_index,
+                         a.NCp + rec.y / a.Cs, *no_lds, bad_page, kFinish, chunks & 0xffff);
     }
     cur = nxt;
     rec = nrec;
@@ -508,7 +503,7 @@ __device__ __forceinline__ void short_suffix_items(const AttnArgs& a, int& bad_p
 // a plain linear read); V as [page][channel][2 halves of 8 slots], the 16-byte unit index u
 // XOR-ed with (u>>3)&1 for the same reason.
 // ---------------------------------------------------------------------------------------
-constexpr int kStepBytes = 2 * kBlockTok * kD * 2;   // K + V of one 32-token step, of an 8-bit cache of one of 64 tokens
+constexpr int kStepBytes = 2 * kBlockTok * kD * 2;   // K + V of one 32-token step
 // prefix items rescale their accumulators only when a lane's eight weights sum to more than this
 constexpr float kMaxWeight = 256.0f;
 // s_waitcnt immediate (gfx9 encoding): vector-memory counter <= vm, LDS/scalar counter <= lgkm
@@ -536,22 +531,15 @@ constexpr int waitcnt_imm(int vm, int lgkm) { return (vm & 0xf) | ((vm >> 4) << 
 // 177 -> 150 us (0.80 PFLOP/s); the 177 us were one workgroup of 8 waves per CU with all of a group's rows,
 // staged through registers and kept in step by one barrier per step.
 constexpr int kPrefixStages = 4;
-template <bool kFp8>
 struct PrefixLds {
   __attribute__((aligned(16))) char buf[kPrefixStages][kStepBytes];
 };
-template <>
-struct PrefixLds<true> {
-  __attribute__((aligned(16))) char buf[kPrefixStages][kStepBytes];
-  __attribute__((aligned(16))) char exponents[kPrefixStages][kWaves][4 * 2 * kPage];   // of the step's four pages, one copy a wave
-};
 typedef const char __attribute__((address_space(1))) * GlobalBytes;
 
-template <bool kHalves, bool kFp8>
+template <bool kHalves>
 __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, const int kvh, const int half,
-                                            PrefixLds<kFp8>& lds, int& bad_page) {
-  typedef KvStep<kFp8> Step;
-  constexpr int NW = 4, MTW = 2, kLoads = kFp8 ? 5 : 4;
+                                            PrefixLds& lds, int& bad_page) {
+  constexpr int NW = 4, MTW = 2, kLoads = 4;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -569,66 +557,43 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
   const int nt = tiles > wave + NW ? 2 : tiles > wave ? 1 : 0;   // wave-uniform: tiles wave, wave + 4
 
   const int32_t* table_row = a.prefix_table + (size_t)g * a.max_pp;
-  const int nsteps = (tok_end - tok_begin + Step::kTok - 1) / Step::kTok;
+  const int nsteps = (tok_end - tok_begin + kBlockTok - 1) / kBlockTok;
   const int first_page = tok_begin >> 4;
   const int last_page = (tok_end - 1) >> 4;
   // Page ids (scalar): fetched an iteration before they are used, checked once per item.  A slot past
   // the end repeats the last page: valid bytes that nobody uses, so that every wait knows how many
   // loads are in flight.
   uint32_t id_max = 0;
-  int r[Step::kPages];
+  int r0, r1;
   auto fetch_ids = [&](int n) {
-#pragma unroll
-    for (int u = 0; u < Step::kPages; ++u) r[u] = ld_uniform(table_row + min(first_page + Step::kPages * n + u, last_page));
+    r0 = ld_uniform(table_row + min(first_page + 2 * n, last_page));
+    r1 = ld_uniform(table_row + min(first_page + 2 * n + 1, last_page));
   };
-  // A step is 1024 16-byte vectors, half of them keys; wave w fills 64 in lane order with each of four loads.
-  //   bf16: K of page 0, K of page 1, V of page 0, V of page 1 (256 each, contiguous in memory); slots 64 w .. + 63 of each region.
-  // K as 32 token rows of 256 B, the 16-byte chunk index XOR-ed with bits 0, 1, 3, 4 of the row; V as [page][channel][2
+  // A step is 1024 16-byte vectors: K of page 0, K of page 1, V of page 0, V of page 1 (256 each,
+  // contiguous in memory); wave w fills slots 64 w .. + 63 of each region, in lane order.  K as 32 token
+  // rows of 256 B, the 16-byte chunk index XOR-ed with bits 0, 1, 3, 4 of the row; V as [page][channel][2
   // halves of 8 slots], the unit index u XOR-ed with (u >> 3) & 1: both are undone on the source side.
-  //   8 bit: K of pages 0 and 1, of 2 and 3, V likewise (128 vectors a page); a load is half a page.  K as 64 token rows of 128 B, the
-  // chunk index XOR-ed with bits 1, 4, 5 of the row (the 16 rows of an operand read differ in bits 0, 1, 4, 5, and two rows span
-  // the banks); V as [page][channel], which 16 lanes read in order.  A fifth load brings the pages' exponents, to each wave.
-  uint32_t src_off[4];
+  uint32_t src_off[kLoads];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if constexpr (kFp8) {
-      const int pos = (wave & 1) * 64 + lane;   // vector of the page
-      const int key = ((pos >> 4) & 1) | (wave >> 1) << 1 | (k & 1) << 2;
-      src_off[k] = 16u * (uint32_t)((k >> 1) ? pos : pos ^ key);
-    } else {
-      const int s_pos = wave * 64 + lane;
-      const int slot = s_pos >> 4;
-      const int key = ((k & 1) << 3) | ((slot >> 3) << 2) | (slot & 3);
-      src_off[k] = 16u * (uint32_t)((k >> 1) ? (s_pos ^ ((s_pos >> 3) & 1)) : ((slot << 4) | ((s_pos & 15) ^ key)));
-    }
+  for (int k = 0; k < kLoads; ++k) {
+    const int s_pos = wave * 64 + lane;
+    const int slot = s_pos >> 4;
+    const int key = ((k & 1) << 3) | ((slot >> 3) << 2) | (slot & 3);
+    src_off[k] = 16u * (uint32_t)((k >> 1) ? (s_pos ^ ((s_pos >> 3) & 1)) : ((slot << 4) | ((s_pos & 15) ^ key)));
   }
   auto issue = [&](uint32_t ring) {
-    uint64_t off[Step::kPages];
+    id_max = max(id_max, max((uint32_t)r0, (uint32_t)r1));
+    const uint32_t p0 = (uint32_t)r0 < (uint32_t)a.num_pages ? r0 : 0, p1 = (uint32_t)r1 < (uint32_t)a.num_pages ? r1 : 0;
+    const uint64_t off0 = ((uint64_t)p0 * (uint32_t)a.Hkv + (uint32_t)kvh) * (kPage * kD * 2);
+    const uint64_t off1 = ((uint64_t)p1 * (uint32_t)a.Hkv + (uint32_t)kvh) * (kPage * kD * 2);
 #pragma unroll
-    for (int u = 0; u < Step::kPages; u += 2) id_max = max(id_max, max((uint32_t)r[u], (uint32_t)r[u + 1]));
-#pragma unroll
-    for (int u = 0; u < Step::kPages; ++u) {
-      const uint32_t page = (uint32_t)r[u] < (uint32_t)a.num_pages ? r[u] : 0;
-      off[u] = ((uint64_t)page * (uint32_t)a.Hkv + (uint32_t)kvh) * Step::kPageBytes;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint64_t page_off = kFp8 ? (wave >> 1 ? off[2 * (k & 1) + 1] : off[2 * (k & 1)]) : off[k & 1];
-      const GlobalBytes base = reinterpret_cast<GlobalBytes>(reinterpret_cast<uintptr_t>((k >> 1) ? a.v_pages : a.k_pages)) + page_off;
+    for (int k = 0; k < kLoads; ++k) {
+      const GlobalBytes base = reinterpret_cast<GlobalBytes>(reinterpret_cast<uintptr_t>((k >> 1) ? a.v_pages : a.k_pages)) +
+                               ((k & 1) ? off1 : off0);
       char* dst = lds.buf[0] + (ring + k * 4096 + wave * 1024);   // wave-uniform; lane l lands at dst + 16 l
       __builtin_amdgcn_global_load_lds(
           reinterpret_cast<const __attribute__((address_space(1))) void*>(base + src_off[k]),
           reinterpret_cast<__attribute__((address_space(3))) void*>((uint32_t)reinterpret_cast<uintptr_t>(dst)), 16, 0, kHalves ? 0 : 2);   // (2: non-temporal)
-    }
-    if constexpr (kFp8) {
-      if (lane < 8) {   // lane 2 u + x: the keys' (x = 0) or the values' exponents of page u
-        const uint64_t page_off = lane < 4 ? (lane < 2 ? off[0] : off[1]) : (lane < 6 ? off[2] : off[3]);
-        const GlobalBytes src = reinterpret_cast<GlobalBytes>(reinterpret_cast<uintptr_t>(a.exponents)) + (page_off >> 6) + (lane & 1) * kPage;
-        char* dst = lds.exponents[0][0] + (ring / kStepBytes * kWaves + wave) * (4 * 2 * kPage);
-        __builtin_amdgcn_global_load_lds(
-            reinterpret_cast<const __attribute__((address_space(1))) void*>(src),
-            reinterpret_cast<__attribute__((address_space(3))) void*>((uint32_t)reinterpret_cast<uintptr_t>(dst)), 16, 0, 0);
-      }
     }
   };
   constexpr uint32_t kRingBytes = kPrefixStages * kStepBytes;
@@ -656,7 +621,7 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
       u32x4 v = {0u, 0u, 0u, 0u};
-      if (idx >= 0) v = *reinterpret_cast<const u32x4*>(a.q + (size_t)idx * kD + Step::channel(kk, j));
+      if (idx >= 0) v = *reinterpret_cast<const u32x4*>(a.q + (size_t)idx * kD + (4 * kk + j) * 8);
       v ^= sign_flip;
       qreg[qt][kk] = v;
     }
@@ -678,38 +643,28 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
     for (int ct = 0; ct < 8; ++ct) acc[qt][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int k_rd = kFp8 ? (16 * (i >> 2) + (i & 3)) * 128 : (8 * (i >> 2) + (i & 3)) * 256;
-  const int k_key = kFp8 ? i >> 1 : i;
-  const int v_rd = 2 * kBlockTok * kD + (kFp8 ? 128 * 16 * j + 16 * i : (j >> 1) * 4096 + (((2 * i + (j & 1)) ^ ((i >> 2) & 1)) << 4));
+  const int k_rd = (8 * (i >> 2) + (i & 3)) * 256;
+  const int v_rd = 2 * kBlockTok * kD + (j >> 1) * 4096 + (((2 * i + (j & 1)) ^ ((i >> 2) & 1)) << 4);
   auto run = [&](auto nt_tag) {
     constexpr int NTraw = decltype(nt_tag)::value;
     constexpr int NT = NTraw > 0 ? NTraw : 1;   // (no zero-length arrays; a wave without tiles only moves data)
-    u32x4 kr[Step::kTiles][Step::kKeyLoads], vr[8], kx, vx;
+    u32x4 kr[2][4], vr[8];
     auto read_k = [&](uint32_t ring) {
 #pragma unroll
-      for (int T = 0; T < Step::kTiles; ++T)
+      for (int T = 0; T < 2; ++T)
 #pragma unroll
-        for (int kk = 0; kk < Step::kKeyLoads; ++kk)
-          kr[T][kk] = *reinterpret_cast<const u32x4*>(lds.buf[0] + ring + k_rd + T * 4 * Step::kRowBytes + (((4 * kk + j) ^ k_key) << 4));
-      if constexpr (kFp8)
-        kx = *reinterpret_cast<const u32x4*>(lds.exponents[0][0] + (ring / kStepBytes * kWaves + wave) * (4 * 2 * kPage) + (i >> 2) * (2 * kPage));
-    };
-    auto read_v = [&](uint32_t ring) {
-#pragma unroll
-      for (int ct = 0; ct < 8; ++ct) vr[ct] = *reinterpret_cast<const u32x4*>(lds.buf[0] + ring + v_rd + ct * (16 * kPage * (kFp8 ? 1 : 2)));
-      if constexpr (kFp8)
-        vx = *reinterpret_cast<const u32x4*>(lds.exponents[0][0] + (ring / kStepBytes * kWaves + wave) * (4 * 2 * kPage) + j * (2 * kPage) + kPage);
+        for (int kk = 0; kk < 4; ++kk)
+          kr[T][kk] = *reinterpret_cast<const u32x4*>(lds.buf[0] + ring + k_rd + T * 4 * 256 + (((4 * kk + j) ^ i) << 4));
     };
     // slot 0 has landed when at most the two younger slots' loads are in flight
     __builtin_amdgcn_s_waitcnt(waitcnt_imm(2 * kLoads, 15));
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if constexpr (NTraw > 0 && !kFp8) read_k(0);
+    if constexpr (NTraw > 0) read_k(0);
     uint32_t ring = 0;
     auto iteration = [&](auto last_tag, int n) {
       constexpr bool kLast = decltype(last_tag)::value;
-      if constexpr (NTraw > 0 && kFp8) read_k(ring);         // (slot n is there since the last barrier)
       __builtin_amdgcn_s_waitcnt(waitcnt_imm(kLoads, 15));   // slot n+1 has landed
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_barrier();                          // ... for every wave; all have read V(n-1)
@@ -717,51 +672,37 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
       issue((ring + 3 * kStepBytes) & (kRingBytes - 1));
       if constexpr (NTraw == 0) fetch_ids(n + 4);
       if constexpr (NTraw > 0) {
-        if constexpr (!kFp8) read_v(ring);
-        f32x4 s[NT][Step::kTiles];
 #pragma unroll
-        for (int qt = 0; qt < NT; ++qt)
+        for (int ct = 0; ct < 8; ++ct) vr[ct] = *reinterpret_cast<const u32x4*>(lds.buf[0] + ring + v_rd + ct * (16 * kPage * 2));
+        f32x4 s[NT][2];
 #pragma unroll
-          for (int T = 0; T < Step::kTiles; ++T) s[qt][T] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if constexpr (kFp8) {
+        for (int qt = 0; qt < NT; ++qt) s[qt][0] = s[qt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int T = 0; T < Step::kTiles; ++T) {
-            const float scale = key_scale(kx, T, i);
+        for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-              const u32x4 k = bf16_of_codes(kr[T][kk >> 1][2 * (kk & 1)], kr[T][kk >> 1][2 * (kk & 1) + 1], scale);
-#pragma unroll
-              for (int qt = 0; qt < NT; ++qt) s[qt][T] = mfma_16x16x32(k, qreg[qt][kk], s[qt][T]);
-            }
+          for (int qt = 0; qt < NT; ++qt) {
+            s[qt][0] = mfma_16x16x32(kr[0][kk], qreg[qt][kk], s[qt][0]);
+            s[qt][1] = mfma_16x16x32(kr[1][kk], qreg[qt][kk], s[qt][1]);
           }
-        } else {
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-            for (int qt = 0; qt < NT; ++qt) {
-              s[qt][0] = mfma_16x16x32(kr[0][kk], qreg[qt][kk], s[qt][0]);
-              s[qt][1] = mfma_16x16x32(kr[1][kk], qreg[qt][kk], s[qt][1]);
-            }
-        }
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (kFp8) read_v(ring);
-        else if constexpr (!kLast) read_k((ring + kStepBytes) & (kRingBytes - 1));
+        if constexpr (!kLast) read_k((ring + kStepBytes) & (kRingBytes - 1));
         fetch_ids(n + 4);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kLast) {
-          const int t0 = tok_begin + n * Step::kTok;
-          if (t0 + Step::kTok > tok_end) {   // wave-uniform: the ragged end of the chunk
+          const int t0 = tok_begin + n * kBlockTok;
+          if (t0 + kBlockTok > tok_end) {   // wave-uniform: the ragged end of the chunk
 #pragma unroll
             for (int qt = 0; qt < NT; ++qt)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int T = 0; T < Step::kTiles; ++T)
-                  if (t0 + Step::kLaneTok * j + 4 * T + e >= tok_end) s[qt][T][e] = -INFINITY;
+              for (int e = 0; e < 4; ++e) {
+                if (t0 + 8 * j + e >= tok_end) s[qt][0][e] = -INFINITY;
+                if (t0 + 8 * j + 4 + e >= tok_end) s[qt][1][e] = -INFINITY;
+              }
             // value slots no token owns may hold anything (NaN included): zero them
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-              const uint32_t mask = value_mask<kFp8>(t0 + Step::kLaneTok * j, tok_end, d);
+              const int tok = t0 + 8 * j + 2 * d;
+              const uint32_t mask = (tok < tok_end ? 0x0000ffffu : 0u) | (tok + 1 < tok_end ? 0xffff0000u : 0u);
 #pragma unroll
               for (int ct = 0; ct < 8; ++ct) vr[ct][d] &= mask;
             }
@@ -769,36 +710,25 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
         }
 #pragma unroll
         for (int qt = 0; qt < NT; ++qt) {
-          u32x4 pb[Step::kHalves];
+          u32x4 pb;
           float psum;
           auto weights = [&] {
-            float p[8 * Step::kHalves], sums[Step::kHalves];
+            float p[8];
 #pragma unroll
-            for (int h = 0; h < Step::kHalves; ++h) {
-              float* ph = p + 8 * h;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                ph[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][2 * h][e], sc, -m_run[qt]));
-                ph[4 + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][2 * h + 1][e], sc, -m_run[qt]));
-              }
-              pb[h] = weight_operand<kFp8>(ph, kFp8 ? vx[2 * h] : 0u, kFp8 ? vx[2 * h + 1] : 0u);
-              // (256-row blocks of a bf16 cache: the rounded weights, the same that multiply V)
-              if constexpr (kHalves && !kFp8) sums[h] = sum_bf16(pb[h]);
-              else sums[h] = ((ph[0] + ph[1]) + (ph[2] + ph[3])) + ((ph[4] + ph[5]) + (ph[6] + ph[7]));
+            for (int e = 0; e < 4; ++e) {
+              p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][0][e], sc, -m_run[qt]));
+              p[4 + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][1][e], sc, -m_run[qt]));
             }
-            psum = sums[0];
-            if constexpr (kFp8) psum += sums[1];
+            pb = u32x4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
+            // (256-row blocks: the rounded weights, the same that multiply V)
+            if constexpr (kHalves) psum = sum_bf16(pb);
+            else psum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
           };
           auto move_reference = [&] {
-            float mx[Step::kHalves];
-#pragma unroll
-            for (int h = 0; h < Step::kHalves; ++h) {
-              const f32x4 s0 = s[qt][2 * h], s1 = s[qt][2 * h + 1];
-              mx[h] = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])),
-                            fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));   // this lane's tokens
-            }
-            if constexpr (kFp8) mx[0] = fmaxf(mx[0], mx[1]);
-            const float m_new = fmaxf(m_run[qt], rows_allreduce_max(mx[0]) * sc);
+            const f32x4 s0 = s[qt][0], s1 = s[qt][1];
+            const float mx = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])),
+                                   fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));   // this lane's 8 tokens
+            const float m_new = fmaxf(m_run[qt], rows_allreduce_max(mx) * sc);
             if (kHalves || __builtin_amdgcn_ballot_w64(m_new > m_run[qt]) != 0) {      // wave-uniform
               const float alpha = __builtin_amdgcn_exp2f(m_run[qt] - m_new);           // 1 where the row did not move
               l_run[qt] *= alpha;
@@ -819,9 +749,7 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
           }
           l_run[qt] += psum;
 #pragma unroll
-          for (int ct = 0; ct < 8; ++ct)
-#pragma unroll
-            for (int h = 0; h < Step::kHalves; ++h) acc[qt][ct] = mfma_16x16x32(value_operand<kFp8>(vr[ct], h), pb[h], acc[qt][ct]);
+          for (int ct = 0; ct < 8; ++ct) acc[qt][ct] = mfma_16x16x32(vr[ct], pb, acc[qt][ct]);
         }
       }
       ring = (ring + kStepBytes) & (kRingBytes - 1);
@@ -853,9 +781,9 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
 
 // Two shapes: blocks of 128 query rows, or, for groups with more than 128 rows, blocks of 256 rows whose
 // halves are taken separately; both with workgroups of 4 waves, two per CU.
-template <bool kWide, bool kFp8>
+template <bool kWide>
 __device__ __forceinline__ void prefix_kernel_body(const AttnArgs& a) {
-  __shared__ PrefixLds<kFp8> lds;
+  __shared__ PrefixLds lds;
   __shared__ int next_item;
   const int n_work = a.counters[MARL_CTR_NUM_PREFIX_ITEMS] * a.Hkv;
   // wide: entries of the queue come in groups of 16, the first halves of eight (item, KV head) pairs and
@@ -868,7 +796,7 @@ __device__ __forceinline__ void prefix_kernel_body(const AttnArgs& a) {
   // expensive at the tail of a kernel, where only a few workgroups are left.
   // (skipped when the plan found no such item: the scan of the short entries is a chain of
   // dependent loads at the very start of the kernel)
-  if (a.counters[MARL_CTR_NUM_SHORT_PARTIAL_ITEMS] > 0) short_suffix_items<false, kFp8>(a, bad_page);
+  if (a.counters[MARL_CTR_NUM_SHORT_PARTIAL_ITEMS] > 0) short_suffix_items<false>(a, bad_page);
   __syncthreads();
   for (bool first = true;; first = false) {   // first item = block index, as in the suffix kernel
     int qi = blockIdx.x;
@@ -884,23 +812,19 @@ __device__ __forceinline__ void prefix_kernel_body(const AttnArgs& a) {
       const int pair = (qi >> 4) * 8 + (qi & 7);
       if (pair >= n_work) continue;           // workgroup-uniform
       const int4 it = a.prefix_items[pair / a.Hkv];
-      prefix_item<true, kFp8>(a, it, pair % a.Hkv, (qi >> 3) & 1, lds, bad_page);
+      prefix_item<true>(a, it, pair % a.Hkv, (qi >> 3) & 1, lds, bad_page);
     } else {
       const int4 it = a.prefix_items[qi / a.Hkv];
-      prefix_item<false, kFp8>(a, it, qi % a.Hkv, 0, lds, bad_page);
+      prefix_item<false>(a, it, qi % a.Hkv, 0, lds, bad_page);
     }
   }
   if (bad_page) atomicOr(&a.counters[MARL_CTR_FLAGS], MARL_FLAG_BAD_PAGE);
 }
 
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void prefix_kernel(AttnArgs a) { prefix_kernel_body<false, false>(a); }
+void prefix_kernel(AttnArgs a) { prefix_kernel_body<false>(a); }
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void prefix_kernel_wide(AttnArgs a) { prefix_kernel_body<true, false>(a); }
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void prefix_fp8_kernel(AttnArgs a) { prefix_kernel_body<false, true>(a); }
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void prefix_fp8_kernel_wide(AttnArgs a) { prefix_kernel_body<true, true>(a); }
+void prefix_kernel_wide(AttnArgs a) { prefix_kernel_body<true>(a); }
 
 // ---------------------------------------------------------------------------------------
 // Items kernel: prefix and suffix items of calls of up to kOneQueueItems (sequence, KV head) pairs in one launch.
@@ -918,9 +842,9 @@ void prefix_fp8_kernel_wide(AttnArgs a) { prefix_kernel_body<true, true>(a); }
 // 72 us for the attention of the batch above, up to three times the time where groups are large.  Two steps in
 // flight per wave, for which there are registers: 2-3 % slower, by batches of short items.)
 // ---------------------------------------------------------------------------------------
-template <bool kWide, bool kFp8>
+template <bool kWide>
 __device__ __forceinline__ void items_kernel_body(const AttnArgs& a) {
-  __shared__ union { PrefixLds<kFp8> ring; ItemLds<1> item; } lds;
+  __shared__ union { PrefixLds ring; ItemLds<1> item; } lds;
   __shared__ int next_item;
   const int n_long = a.counters[MARL_CTR_NUM_LONG_SUFFIX_ITEMS] * a.Hkv;
   const int pairs = a.counters[MARL_CTR_NUM_PREFIX_ITEMS] * a.Hkv;
@@ -937,15 +861,15 @@ __device__ __forceinline__ void items_kernel_body(const AttnArgs& a) {
   const int head = a.counters[MARL_CTR_NUM_FIRST_SUFFIX_ITEMS] * a.Hkv;
   const int i = threadIdx.x & 15;
   int bad_page = 0;
-  if (partials && !as_entries) short_suffix_items<false, kFp8>(a, bad_page);
+  if (partials && !as_entries) short_suffix_items<false>(a, bad_page);
   for (int e = blockIdx.x; e < n_prefix + n_suffix;) {   // workgroup-uniform
     if (e >= head && e < head + n_prefix) {
       const int qi = e - head;
       if constexpr (kWide) {
         const int pair = (qi >> 4) * 8 + (qi & 7);
-        if (pair < pairs) prefix_item<true, kFp8>(a, a.prefix_items[pair / a.Hkv], pair % a.Hkv, (qi >> 3) & 1, lds.ring, bad_page);
+        if (pair < pairs) prefix_item<true>(a, a.prefix_items[pair / a.Hkv], pair % a.Hkv, (qi >> 3) & 1, lds.ring, bad_page);
       } else {
-        prefix_item<false, kFp8>(a, a.prefix_items[qi / a.Hkv], qi % a.Hkv, 0, lds.ring, bad_page);
+        prefix_item<false>(a, a.prefix_items[qi / a.Hkv], qi % a.Hkv, 0, lds.ring, bad_page);
       }
     } else {
       const int qi = e < head ? e : e - n_prefix;
@@ -955,8 +879,8 @@ __device__ __forceinline__ void items_kernel_body(const AttnArgs& a) {
       const int row_index[1] = {i < a.R ? s * a.Hq + kvh * a.R + i : -1};
       const int chunks = ld_uniform(a.seq_chunks + s);
       if (qi < n_long || chunks >> 16 != 1)
-        process_item<1, kSuffixWaves, kFp8>(a, a.suffix_table + (size_t)s * a.max_sp, it.y, it.z, kvh, row_index,
-                                            a.NCp + it.y / a.Cs, lds.item, bad_page, chunks == 1 << 16, 0);
+        process_item<1, kSuffixWaves>(a, a.suffix_table + (size_t)s * a.max_sp, it.y, it.z, kvh, row_index,
+                                      a.NCp + it.y / a.Cs, lds.item, bad_page, chunks == 1 << 16, 0);
     }
     if (n_prefix + n_suffix <= (int)gridDim.x) break;   // every item has a workgroup of its own
     if (threadIdx.x == 0) next_item = gridDim.x + atomicAdd(&a.counters[MARL_CTR_SUFFIX_CURSOR], 1);
@@ -969,13 +893,9 @@ __device__ __forceinline__ void items_kernel_body(const AttnArgs& a) {
 
 static_assert(kSuffixWaves == 4, "prefix and suffix items share workgroups");
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void items_kernel(AttnArgs a) { items_kernel_body<false, false>(a); }
+void items_kernel(AttnArgs a) { items_kernel_body<false>(a); }
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void items_kernel_wide(AttnArgs a) { items_kernel_body<true, false>(a); }
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void items_fp8_kernel(AttnArgs a) { items_kernel_body<false, true>(a); }
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void items_fp8_kernel_wide(AttnArgs a) { items_kernel_body<true, true>(a); }
+void items_kernel_wide(AttnArgs a) { items_kernel_body<true>(a); }
 
 // ---------------------------------------------------------------------------------------
 // Merge kernel: the second reduction of split-KV decode attention.  For every (sequence,
@@ -996,10 +916,9 @@ void items_fp8_kernel_wide(AttnArgs a) { items_kernel_body<true, true>(a); }
 // ---------------------------------------------------------------------------------------
 constexpr int kMergeThreads = 256;
 constexpr int kRowsPerBlock = kMergeThreads / 32;
-constexpr int kEager = 4;   // partials fetched up front
 
-template <bool kFp8>
-__device__ __forceinline__ void merge_kernel_body(const AttnArgs& a) {
+__global__ __launch_bounds__(kMergeThreads) __attribute__((amdgpu_waves_per_eu(3, 3)))
+void merge_kernel(AttnArgs a) {
   // (the row's chunk counts are requested before the short items: most workgroups have none of these, and
   // where every row is finished with them a workgroup is one load long instead of two)
   const int row = blockIdx.x * kRowsPerBlock + (threadIdx.x >> 5);
@@ -1009,106 +928,50 @@ __device__ __forceinline__ void merge_kernel_body(const AttnArgs& a) {
   // the merge with the group's prefix partials in one go, one item per wave
   {
     int bad_page = 0;
-    short_suffix_items<true, kFp8>(a, bad_page);
+    short_suffix_items<true>(a, bad_page);
     if (bad_page) atomicOr(&a.counters[MARL_CTR_FLAGS], MARL_FLAG_BAD_PAGE);
   }
-  const int sub = threadIdx.x & 31;   // lane within the half wave: channels 4*sub .. 4*sub+3
   const int npc = info & 0xffff, nsc = info >> 16;
   // a sequence whose own tokens are one item was finished where that item was processed: above
   // (at most kShortTokens tokens) or in the suffix kernel; the items kernel finishes only those without a prefix
   if (nsc == 1 && (npc == 0 || own <= kShortTokens)) return;
-  const int n = npc + nsc;
-  const int nslot = a.NCp + a.NCs;
-  const float2* ml = a.partial_ml + (size_t)row * nslot;
-  const float* po = a.partial_o + (size_t)row * nslot * kD + 4 * sub;
-  auto slot_of = [&](int k) { return k < npc ? k : a.NCp + (k - npc); };
-
-  float2 mlk[kEager];
-  f32x4 ok[kEager];
-#pragma unroll
-  for (int k = 0; k < kEager; ++k) {
-    mlk[k] = make_float2(-INFINITY, 0.f);
-    ok[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (k < n) {
-      const int sl = slot_of(k);
-      mlk[k] = ml[sl];
-      ok[k] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(po + (size_t)sl * kD));
-    }
-  }
-  float mstar = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < kEager; ++k) mstar = fmaxf(mstar, mlk[k].x);
-  for (int k = kEager; k < n; k += kMaximaAtOnce) {
-    float mk[kMaximaAtOnce];
-#pragma unroll
-    for (int u = 0; u < kMaximaAtOnce; ++u) mk[u] = ml[slot_of(min(k + u, n - 1))].x;
-#pragma unroll
-    for (int u = 0; u < kMaximaAtOnce; ++u) mstar = fmaxf(mstar, mk[u]);
-  }
-
-  float denom = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int k = 0; k < kEager; ++k) {
-    const float f = (mlk[k].x == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(mlk[k].x - mstar);
-    denom = __builtin_fmaf(mlk[k].y, f, denom);
-    acc += ok[k] * f;
-  }
-  for (int k = kEager; k < n; k += kEager) {   // as many at once as before the first use
-#pragma unroll
-    for (int u = 0; u < kEager; ++u) {
-      const int sl = slot_of(min(k + u, n - 1));
-      mlk[u] = ml[sl];
-      ok[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(po + (size_t)sl * kD));
-    }
-#pragma unroll
-    for (int u = 0; u < kEager; ++u) {
-      const float f = (mlk[u].x == -INFINITY || k + u >= n) ? 0.f : __builtin_amdgcn_exp2f(mlk[u].x - mstar);
-      denom = __builtin_fmaf(mlk[u].y, f, denom);
-      acc += ok[u] * f;
-    }
-  }
-  f32x4 r = {0.f, 0.f, 0.f, 0.f};
-  if (n > 0 && denom > 0.f) r = acc * (1.0f / denom);
-  if (a.out_dtype == MARL_OUT_F32) {
-    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + (size_t)row * kD + 4 * sub) = r;
-  } else {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    const bf16x4 v = {(__bf16)r[0], (__bf16)r[1], (__bf16)r[2], (__bf16)r[3]};
-    *reinterpret_cast<bf16x4*>(reinterpret_cast<uint16_t*>(a.out) + (size_t)row * kD + 4 * sub) = v;
-  }
-}
-
-__global__ __launch_bounds__(kMergeThreads) __attribute__((amdgpu_waves_per_eu(3, 3)))
-void merge_kernel(AttnArgs a) { merge_kernel_body<false>(a); }
-__global__ __launch_bounds__(kMergeThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void merge_fp8_kernel(AttnArgs a) { merge_kernel_body<true>(a); }
-
-typedef void (*AttnKernel)(AttnArgs);
-AttnKernel prefix_kernel_of(bool wide, bool fp8) { return fp8 ? (wide ? prefix_fp8_kernel_wide : prefix_fp8_kernel) : (wide ? prefix_kernel_wide : prefix_kernel); }
-AttnKernel items_kernel_of(bool wide, bool fp8) { return fp8 ? (wide ? items_fp8_kernel_wide : items_fp8_kernel) : (wide ? items_kernel_wide : items_kernel); }
-int blocks_per_cu(AttnKernel kernel, int threads) {
-  int n = 0;
-  if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, reinterpret_cast<const void*>(kernel), threads, 0) != hipSuccess || n < 1) n = 1;
-  return n;
+  merge_row(a, row, npc, nsc);
 }
 
 }  // namespace
 
-int prefix_blocks_per_cu(bool wide, bool fp8) { return blocks_per_cu(prefix_kernel_of(wide, fp8), 256); }
-int items_blocks_per_cu(bool wide, bool fp8) { return blocks_per_cu(items_kernel_of(wide, fp8), 256); }
-int suffix_blocks_per_cu(bool fp8) { return blocks_per_cu(fp8 ? suffix_fp8_kernel : suffix_kernel, kSuffixWaves * 64); }
+int prefix_blocks_per_cu(bool wide) {
+  int n = 0;
+  const hipError_t e = wide ? hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, prefix_kernel_wide, 256, 0)
+                            : hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, prefix_kernel, 256, 0);
+  if (e != hipSuccess || n < 1) n = 1;
+  return n;
+}
+int items_blocks_per_cu(bool wide) {
+  int n = 0;
+  const hipError_t e = wide ? hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, items_kernel_wide, 256, 0)
+                            : hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, items_kernel, 256, 0);
+  if (e != hipSuccess || n < 1) n = 1;
+  return n;
+}
+int suffix_blocks_per_cu() {
+  int n = 0;
+  if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, suffix_kernel, kSuffixWaves * 64, 0) != hipSuccess || n < 1) n = 1;
+  return n;
+}
 
 hipError_t launch_prefix(const AttnArgs& a, int grid, hipStream_t st) {
-  hipLaunchKernelGGL(prefix_kernel_of(a.qblock_rows == kRowsPerQBlockWide, a.exponents != nullptr), dim3(grid), dim3(256), 0, st, a);
+  if (a.qblock_rows == 256) hipLaunchKernelGGL(prefix_kernel_wide, dim3(grid), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(prefix_kernel, dim3(grid), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_suffix(const AttnArgs& a, int grid, hipStream_t st) {
-  hipLaunchKernelGGL(a.exponents ? suffix_fp8_kernel : suffix_kernel, dim3(grid), dim3(kSuffixWaves * 64), 0, st, a);
+  hipLaunchKernelGGL(suffix_kernel, dim3(grid), dim3(kSuffixWaves * 64), 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_items(const AttnArgs& a, int grid, hipStream_t st) {
-  hipLaunchKernelGGL(items_kernel_of(a.qblock_rows == kRowsPerQBlockWide, a.exponents != nullptr), dim3(grid), dim3(256), 0, st, a);
+  if (a.qblock_rows == kRowsPerQBlockWide) hipLaunchKernelGGL(items_kernel_wide, dim3(grid), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(items_kernel, dim3(grid), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_merge(const AttnArgs& a, hipStream_t st) {
@@ -1117,7 +980,7 @@ hipError_t launch_merge(const AttnArgs& a, hipStream_t st) {
   // (a wave for every short item: with one head per KV head there are more of those than waves of rows, and a wave took two,
   // one after the other: 209 sequences of up to 76 tokens, 4 / 4 heads, 48.2 us for the call, now 41.1)
   const long grid = std::max((rows + kRowsPerBlock - 1) / kRowsPerBlock, ((long)a.NS * a.Hkv + kWaves - 1) / kWaves);
-  hipLaunchKernelGGL(a.exponents ? merge_fp8_kernel : merge_kernel, dim3((unsigned)grid), dim3(kMergeThreads), 0, st, a);
+  hipLaunchKernelGGL(merge_kernel, dim3((unsigned)grid), dim3(kMergeThreads), 0, st, a);
   return hipGetLastError();
 }
 

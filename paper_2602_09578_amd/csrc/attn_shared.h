@@ -1,0 +1,121 @@
+// What the decode attention kernels over a bf16 cache and over an 8-bit one have in common: how partial results are added and
+// stored, and which workgroup of a small call takes what.
+#ifndef MARL_ATTN_SHARED_H
+#define MARL_ATTN_SHARED_H
+#include "marl_internal.h"
+#include "wave_ops.h"
+
+namespace marl {
+
+constexpr int kAccRowFloats = kD + 4;   // of a row in LDS (the 16 rows that a wave instruction writes start in different banks)
+constexpr int kMaximaAtOnce = 8;        // of partials that are about to be added
+constexpr int kEager = 4;               // partials of a row that are requested before the first is used
+constexpr int kSeqBlock = 8;            // sequences whose workgroups for one KV head and part run on one XCD
+
+// Four channels of a final row.
+__device__ __forceinline__ void store_row_piece(const AttnArgs& a, size_t at, f32x4 v) {
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  if (a.out_dtype == MARL_OUT_F32) {
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = v;
+  } else {
+    *reinterpret_cast<bf16x4*>(reinterpret_cast<uint16_t*>(a.out) + at) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+  }
+}
+
+// Adds the partials of one row, those of npc prefix chunks and nsc own ones, in slot order, and stores the row; half a wave a row.
+__device__ __forceinline__ void merge_row(const AttnArgs& a, const int row, const int npc, const int nsc) {
+  const int sub = threadIdx.x & 31;   // lane within the half wave: channels 4*sub .. 4*sub+3
+  const int n = npc + nsc;
+  const int nslot = a.NCp + a.NCs;
+  const float2* ml = a.partial_ml + (size_t)row * nslot;
+  const float* po = a.partial_o + (size_t)row * nslot * kD + 4 * sub;
+  auto slot_of = [&](int k) { return k < npc ? k : a.NCp + (k - npc); };
+
+  float2 mlk[kEager];
+  f32x4 ok[kEager];
+#pragma unroll
+  for (int k = 0; k < kEager; ++k) {
+    mlk[k] = make_float2(-INFINITY, 0.f);
+    ok[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (k < n) {
+      const int sl = slot_of(k);
+      mlk[k] = ml[sl];
+      ok[k] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(po + (size_t)sl * kD));
+    }
+  }
+  float mstar = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kEager; ++k) mstar = fmaxf(mstar, mlk[k].x);
+  for (int k = kEager; k < n; k += kMaximaAtOnce) {
+    float mk[kMaximaAtOnce];
+#pragma unroll
+    for (int u = 0; u < kMaximaAtOnce; ++u) mk[u] = ml[slot_of(min(k + u, n - 1))].x;
+#pragma unroll
+    for (int u = 0; u < kMaximaAtOnce; ++u) mstar = fmaxf(mstar, mk[u]);
+  }
+
+  float denom = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kEager; ++k) {
+    const float f = (mlk[k].x == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(mlk[k].x - mstar);
+    denom = __builtin_fmaf(mlk[k].y, f, denom);
+    acc += ok[k] * f;
+  }
+  for (int k = kEager; k < n; k += kEager) {   // as many at once as before the first use
+#pragma unroll
+    for (int u = 0; u < kEager; ++u) {
+      const int sl = slot_of(min(k + u, n - 1));
+      mlk[u] = ml[sl];
+      ok[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(po + (size_t)sl * kD));
+    }
+#pragma unroll
+    for (int u = 0; u < kEager; ++u) {
+      const float f = (mlk[u].x == -INFINITY || k + u >= n) ? 0.f : __builtin_amdgcn_exp2f(mlk[u].x - mstar);
+      denom = __builtin_fmaf(mlk[u].y, f, denom);
+      acc += ok[u] * f;
+    }
+  }
+  f32x4 r = {0.f, 0.f, 0.f, 0.f};
+  if (n > 0 && denom > 0.f) r = acc * (1.0f / denom);
+  if (a.out_dtype == MARL_OUT_F32) {
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + (size_t)row * kD + 4 * sub) = r;
+  } else {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    const bf16x4 v = {(__bf16)r[0], (__bf16)r[1], (__bf16)r[2], (__bf16)r[3]};
+    *reinterpret_cast<bf16x4*>(reinterpret_cast<uint16_t*>(a.out) + (size_t)row * kD + 4 * sub) = v;
+  }
+}
+
+// Workgroups are dealt to the eight XCDs in turn.  The workgroups of eight neighbouring sequences (usually samples of
+// one prompt) for one KV head and part follow each other on one XCD, so that the prefix they share is read out
+// of its L2: 64 groups of 4 samples, 16 / 2 heads, 2304 tokens: 67 -> 41 us against a plain order.  The last block of sequences
+// comes after the others and is as wide as there are sequences left: with empty workgroups for those that are not there, the
+// others met on a few CUs of the XCD (one sequence, 8 KV heads, 131072 tokens: 282 us, now 112; 4 KV heads, 16384: 25.7, now 16.9).
+struct SmallGrid {
+  int units;        // (KV head, part) pairs of a block of sequences
+  int left;         // sequences of the last, narrower block
+  int full_slots;   // of an XCD: workgroups for blocks of kSeqBlock sequences (the last eight units may be past the end)
+  __host__ __device__ SmallGrid(const AttnArgs& a)
+      : units(a.Hkv * a.splits), left(a.NS % kSeqBlock), full_slots((a.NS / kSeqBlock * units + 7) / 8 * kSeqBlock) {}
+  __host__ __device__ int workgroups() const { return 8 * (full_slots + (units + 7) / 8 * left); }
+  // what workgroup `index` takes; whether that is there (the last units may be past the end)
+  __device__ __forceinline__ bool place(const AttnArgs& a, int index, int& s, int& kvh, int& part) const {
+    const int xcd = index & 7, slot = index >> 3;
+    int unit = slot / kSeqBlock * 8 + xcd, first = 0, at = slot % kSeqBlock, end = a.NS - left;
+    if (slot >= full_slots) {   // workgroup-uniform
+      unit = (slot - full_slots) / left * 8 + xcd;
+      at = (slot - full_slots) % left;
+      first = end;
+      end = a.NS;
+    }
+    const int pair = unit / a.splits;
+    part = unit % a.splits;
+    s = first + pair / a.Hkv * kSeqBlock + at;
+    kvh = pair % a.Hkv;
+    return s < end;
+  }
+};
+
+}  // namespace marl
+#endif  // MARL_ATTN_SHARED_H

@@ -17,7 +17,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "kv_step.h"
+#include "attn_shared.h"
 #include "marl_internal.h"
 #include "plan_lds.h"
 #include "wave_ops.h"
@@ -26,8 +26,6 @@ namespace marl {
 namespace {
 
 constexpr int NW = kAttnThreads / 64;
-constexpr int kAccRowFloats = kD + 4;   // (the 16 rows that a wave instruction writes start in different banks)
-constexpr int kSeqBlock = 8;            // sequences whose workgroups for one KV head and part run on one XCD
 
 struct SmallLds {
   float m[NW][16];
@@ -35,19 +33,8 @@ struct SmallLds {
   __attribute__((aligned(16))) float acc[NW][16][kAccRowFloats];
 };
 
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void store_row_piece(const AttnArgs& a, size_t at, f32x4 v) {
-  if (a.out_dtype == MARL_OUT_F32) {
-    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = v;
-  } else {
-    *reinterpret_cast<bf16x4*>(reinterpret_cast<uint16_t*>(a.out) + at) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-  }
-}
-
 // Tokens of part `part` of (sequence s, KV head kvh): final rows, or with several parts partials in slots 0 .. splits - 1.
-template <bool kFp8>
 __device__ __forceinline__ void small_item(const AttnArgs& a, const int s, const int kvh, const int part) {
-  typedef KvStep<kFp8> Step;
   __shared__ SmallLds lds;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -57,12 +44,12 @@ __device__ __forceinline__ void small_item(const AttnArgs& a, const int s, const
 
   const int g = ld_uniform(a.group_of_seq + s);
   const int S = min(max(ld_uniform(a.suffix_lens + s), 0), a.max_sp * kPage);
-  // Q^T operand: lane (i, j) holds the channels of query row i that it holds of the keys
+  // Q^T operand: lane (i, j) holds channels 8*(4*kk + j) .. +8 of query row i
   u32x4 qreg[4];
 #pragma unroll
   for (int kk = 0; kk < 4; ++kk) {
     u32x4 v = {0u, 0u, 0u, 0u};
-    if (i < a.R) v = *reinterpret_cast<const u32x4*>(a.q + ((size_t)s * a.Hq + kvh * a.R + i) * kD + Step::channel(kk, j));
+    if (i < a.R) v = *reinterpret_cast<const u32x4*>(a.q + ((size_t)s * a.Hq + kvh * a.R + i) * kD + (4 * kk + j) * 8);
     qreg[kk] = v ^ sign_flip;
   }
   const bool grouped = (unsigned)g < (unsigned)a.NG;
@@ -70,8 +57,8 @@ __device__ __forceinline__ void small_item(const AttnArgs& a, const int s, const
   const int32_t* prefix_row = a.prefix_table + (size_t)(grouped ? g : 0) * a.max_pp;
   const int32_t* suffix_row = a.suffix_table + (size_t)s * a.max_sp;
   // steps: those of the prefix, then those of the sequence's own tokens
-  const int prefix_steps = (P + Step::kTok - 1) / Step::kTok;
-  const int all_steps = prefix_steps + (S + Step::kTok - 1) / Step::kTok;
+  const int prefix_steps = (P + kBlockTok - 1) / kBlockTok;
+  const int all_steps = prefix_steps + (S + kBlockTok - 1) / kBlockTok;
   const int first_step = (int)((long)all_steps * part / a.splits), steps = (int)((long)all_steps * (part + 1) / a.splits);
 
   f32x4 acc[8];
@@ -79,96 +66,98 @@ __device__ __forceinline__ void small_item(const AttnArgs& a, const int s, const
 #pragma unroll
   for (int ct = 0; ct < 8; ++ct) acc[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  KvRegisters<kFp8, false> kv(a, kvh, i, j);
+  const size_t page_bytes = (size_t)a.Hkv * (kPage * kD * 2);
+  const char* kbase = reinterpret_cast<const char*>(a.k_pages) + (size_t)kvh * (kPage * kD * 2) +
+                      ((8 * ((i >> 2) & 1) + (i & 3)) * (kD * 2) + j * 16);
+  const char* vbase = reinterpret_cast<const char*>(a.v_pages) + (size_t)kvh * (kPage * kD * 2) +
+                      (i * (kPage * 2) + (j & 1) * 16);
   // Page ids (scalar loads) of step k and how many of its tokens exist.  An id outside the pool reads page 0 (the
   // plan's workgroup raises the flag).
-  auto load_pages = [&](int k, int (&p)[Step::kPages], int& tokens) {
+  auto load_pages = [&](int k, int& p0, int& p1, int& tokens) {
     const bool own = k >= prefix_steps;
-    const int t = (own ? k - prefix_steps : k) * Step::kTok;
+    const int t = (own ? k - prefix_steps : k) * kBlockTok;
     const int32_t* row = (own ? suffix_row : prefix_row) + (t >> 4);
     tokens = (own ? S : P) - t;
-    p[0] = ld_uniform(row);
-    if constexpr (kFp8) {
-      const int last = (tokens - 1) >> 4;
+    p0 = ld_uniform(row);
+    p1 = tokens > kPage ? ld_uniform(row + 1) : p0;
+    if ((unsigned)p0 >= (unsigned)a.num_pages) p0 = 0;
+    if ((unsigned)p1 >= (unsigned)a.num_pages) p1 = 0;
+  };
+  u32x4 kr[2][4], vr[8];
+  auto issue_k = [&](int p0, int p1) {
+    const char* kp = kbase + (size_t)(i < 8 ? p0 : p1) * page_bytes;
 #pragma unroll
-      for (int u = 1; u < Step::kPages; ++u) p[u] = ld_uniform(row + min(u, last));
-    } else {
-      p[1] = tokens > kPage ? ld_uniform(row + 1) : p[0];
-    }
+    for (int T = 0; T < 2; ++T)
 #pragma unroll
-    for (int u = 0; u < Step::kPages; ++u)
-      if ((unsigned)p[u] >= (unsigned)a.num_pages) p[u] = 0;
+      for (int kk = 0; kk < 4; ++kk) kr[T][kk] = *reinterpret_cast<const u32x4*>(kp + T * (4 * kD * 2) + kk * 64);
+  };
+  auto issue_v = [&](int p0, int p1) {
+    const char* vp = vbase + (size_t)(j < 2 ? p0 : p1) * page_bytes;
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) vr[ct] = *reinterpret_cast<const u32x4*>(vp + ct * (16 * kPage * 2));
   };
 
   // K registers are refilled for the wave's next step as soon as the score products have consumed them, V
   // registers after the output products; the last step is peeled, so that the loop has no conditional loads.
-  int k = first_step + wave, tokens = 0, next[Step::kPages] = {}, ntokens = 0;
+  int k = first_step + wave, tokens = 0, n0 = 0, n1 = 0, ntokens = 0;
   auto step = [&](auto has_next_tag) {
     constexpr bool kHasNext = decltype(has_next_tag)::value;
-    f32x4 sv[Step::kTiles];
+    f32x4 sv[2];
 #pragma unroll
-    for (int T = 0; T < Step::kTiles; ++T) sv[T] = kv.scores(T, qreg);
-    if constexpr (kHasNext) kv.issue_k(next);
-    if (tokens < Step::kTok) {   // wave-uniform: the end of the prefix or of the own tokens
+    for (int T = 0; T < 2; ++T) {
+      sv[T] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) sv[T] = mfma_16x16x32(kr[T][kk], qreg[kk], sv[T]);
+    }
+    if constexpr (kHasNext) issue_k(n0, n1);
+    if (tokens < kBlockTok) {   // wave-uniform: the end of the prefix or of the own tokens
       // tokens past the end: score -inf (weight 0), and zero their value slots, which may hold anything
 #pragma unroll
-      for (int T = 0; T < Step::kTiles; ++T)
+      for (int T = 0; T < 2; ++T)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (Step::kLaneTok * j + 4 * T + e >= tokens) sv[T][e] = -INFINITY;
+          if (8 * j + 4 * T + e >= tokens) sv[T][e] = -INFINITY;
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        const uint32_t mask = value_mask<kFp8>(Step::kLaneTok * j, tokens, d);
+        const int tok = 8 * j + 2 * d;
+        const uint32_t mask = (tok < tokens ? 0x0000ffffu : 0u) | (tok + 1 < tokens ? 0xffff0000u : 0u);
 #pragma unroll
-        for (int ct = 0; ct < 8; ++ct) kv.vr[ct][d] &= mask;
+        for (int ct = 0; ct < 8; ++ct) vr[ct][d] &= mask;
       }
     }
-    float mx[Step::kHalves];
-#pragma unroll
-    for (int h = 0; h < Step::kHalves; ++h)
-      mx[h] = fmaxf(fmaxf(fmaxf(sv[2 * h][0], sv[2 * h][1]), fmaxf(sv[2 * h][2], sv[2 * h][3])),
-                    fmaxf(fmaxf(sv[2 * h + 1][0], sv[2 * h + 1][1]), fmaxf(sv[2 * h + 1][2], sv[2 * h + 1][3])));
-    if constexpr (kFp8) mx[0] = fmaxf(mx[0], mx[1]);
-    mx[0] = rows_allreduce_max(mx[0]);
-    const float m_new = fmaxf(m_run, mx[0] * sc);
+    float mx = fmaxf(fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[0][2], sv[0][3])),
+                     fmaxf(fmaxf(sv[1][0], sv[1][1]), fmaxf(sv[1][2], sv[1][3])));
+    mx = rows_allreduce_max(mx);
+    const float m_new = fmaxf(m_run, mx * sc);
     const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-    float p[8 * Step::kHalves], psum[Step::kHalves];
+    float p[8];
 #pragma unroll
-    for (int h = 0; h < Step::kHalves; ++h) {
-      float* ph = p + 8 * h;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        ph[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[2 * h][e], sc, -m_new));
-        ph[4 + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[2 * h + 1][e], sc, -m_new));
-      }
-      psum[h] = ((ph[0] + ph[1]) + (ph[2] + ph[3])) + ((ph[4] + ph[5]) + (ph[6] + ph[7]));
+    for (int e = 0; e < 4; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[0][e], sc, -m_new));
+      p[4 + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[1][e], sc, -m_new));
     }
-    if constexpr (kFp8) psum[0] += psum[1];
+    const float psum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {   // wave-uniform
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct) acc[ct] *= alpha;
     }
-    l_run = l_run * alpha + psum[0];
+    l_run = l_run * alpha + psum;
     m_run = m_new;
-    u32x4 pb[Step::kHalves];
+    const u32x4 pb = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
 #pragma unroll
-    for (int h = 0; h < Step::kHalves; ++h) pb[h] = weight_operand<kFp8>(p + 8 * h, kFp8 ? kv.vx[2 * h] : 0u, kFp8 ? kv.vx[2 * h + 1] : 0u);
-#pragma unroll
-    for (int ct = 0; ct < 8; ++ct)
-#pragma unroll
-      for (int h = 0; h < Step::kHalves; ++h) acc[ct] = mfma_16x16x32(value_operand<kFp8>(kv.vr[ct], h), pb[h], acc[ct]);
+    for (int ct = 0; ct < 8; ++ct) acc[ct] = mfma_16x16x32(vr[ct], pb, acc[ct]);
     if constexpr (kHasNext) {
-      kv.issue_v(next);
+      issue_v(n0, n1);
       tokens = ntokens;
       k += NW;
-      if (k + NW < steps) load_pages(k + NW, next, ntokens);
+      if (k + NW < steps) load_pages(k + NW, n0, n1, ntokens);
     }
   };
   if (k < steps) {   // wave-uniform
-    load_pages(k, next, tokens);
-    kv.issue_k(next);
-    kv.issue_v(next);
-    if (k + NW < steps) load_pages(k + NW, next, ntokens);
+    load_pages(k, n0, n1, tokens);
+    issue_k(n0, n1);
+    issue_v(n0, n1);
+    if (k + NW < steps) load_pages(k + NW, n0, n1, ntokens);
     while (k + NW < steps) step(std::true_type{});
     step(std::false_type{});
   }
@@ -208,43 +197,15 @@ __device__ __forceinline__ void small_item(const AttnArgs& a, const int s, const
   }
 }
 
-// Workgroups are dealt to the eight XCDs in turn.  The workgroups of eight neighbouring sequences (usually samples of
-// one prompt) for one KV head and part follow each other on one XCD, so that the prefix they share is read out
-// of its L2: 64 groups of 4 samples, 16 / 2 heads, 2304 tokens: 67 -> 41 us against a plain order.  The last block of sequences
-// comes after the others and is as wide as there are sequences left: with empty workgroups for those that are not there, the
-// others met on a few CUs of the XCD (one sequence, 8 KV heads, 131072 tokens: 282 us, now 112; 4 KV heads, 16384: 25.7, now 16.9).
-struct SmallGrid {
-  int units;        // (KV head, part) pairs of a block of sequences
-  int left;         // sequences of the last, narrower block
-  int full_slots;   // of an XCD: workgroups for blocks of kSeqBlock sequences (the last eight units may be past the end)
-  __host__ __device__ SmallGrid(const AttnArgs& a)
-      : units(a.Hkv * a.splits), left(a.NS % kSeqBlock), full_slots((a.NS / kSeqBlock * units + 7) / 8 * kSeqBlock) {}
-  __host__ __device__ int workgroups() const { return 8 * (full_slots + (units + 7) / 8 * left); }
-};
-
-template <bool kFp8>
-__device__ __forceinline__ void decode_small_body(const AttnArgs& a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 3)))
+void decode_small_kernel(AttnArgs a) {
   if (blockIdx.x == 0) {
     plan_in_lds<kAttnThreads, kSmallAttnSeqs, kSmallAttnSeqs, int, true>(a);
     return;
   }
-  const SmallGrid g(a);
-  const int xcd = (blockIdx.x - 1) & 7, slot = (blockIdx.x - 1) >> 3;
-  int unit = slot / kSeqBlock * 8 + xcd, first = 0, at = slot % kSeqBlock, end = a.NS - g.left;
-  if (slot >= g.full_slots) {   // workgroup-uniform
-    unit = (slot - g.full_slots) / g.left * 8 + xcd;
-    at = (slot - g.full_slots) % g.left;
-    first = end;
-    end = a.NS;
-  }
-  const int part = unit % a.splits, pair = unit / a.splits;
-  const int s = first + pair / a.Hkv * kSeqBlock + at;
-  if (s < end) small_item<kFp8>(a, s, pair % a.Hkv, part);   // (the last units may be past the end)
+  int s, kvh, part;
+  if (SmallGrid(a).place(a, blockIdx.x - 1, s, kvh, part)) small_item(a, s, kvh, part);   // (the last units may be past the end)
 }
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 3)))
-void decode_small_kernel(AttnArgs a) { decode_small_body<false>(a); }
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 3)))
-void decode_small_fp8_kernel(AttnArgs a) { decode_small_body<true>(a); }
 
 // Parts of a row added in their order (half a wave per row): the formula of the general merge kernel.
 __global__ __launch_bounds__(kAttnThreads) void merge_parts_kernel(AttnArgs a) {
@@ -309,7 +270,7 @@ int small_attn_splits(const AttnArgs& a) {
 
 hipError_t launch_small_attn(const AttnArgs& a, hipStream_t st) {
   const int grid = SmallGrid(a).workgroups() + 1;   // (at most 65536 pairs and 1536 parts: see above)
-  hipLaunchKernelGGL(a.exponents ? decode_small_fp8_kernel : decode_small_kernel, dim3(grid), dim3(kAttnThreads), 0, st, a);
+  hipLaunchKernelGGL(decode_small_kernel, dim3(grid), dim3(kAttnThreads), 0, st, a);
   return hipGetLastError();
 }
 

@@ -66,9 +66,14 @@ hipError_t launch_merge(const AttnArgs& a, hipStream_t st);
 int small_attn_splits(const AttnArgs& a);
 hipError_t launch_small_attn(const AttnArgs& a, hipStream_t st);
 hipError_t launch_merge_parts(const AttnArgs& a, hipStream_t st);
-int prefix_blocks_per_cu(bool wide, bool fp8);
-int items_blocks_per_cu(bool wide, bool fp8);
-int suffix_blocks_per_cu(bool fp8);
+int prefix_blocks_per_cu(bool wide);
+int items_blocks_per_cu(bool wide);
+int suffix_blocks_per_cu();
+// Over an 8-bit cache: after the plan the items and the merge, or a small call as above (merge_parts is the same).
+hipError_t launch_items_fp8(const AttnArgs& a, int grid, hipStream_t st);
+hipError_t launch_merge_fp8(const AttnArgs& a, hipStream_t st);
+hipError_t launch_small_attn_fp8(const AttnArgs& a, hipStream_t st);
+int items_fp8_blocks_per_cu(bool wide);
 
 struct KvAppendArgs {
   const uint16_t* k_new;
