@@ -125,18 +125,22 @@ __device__ __forceinline__ SuffixItem suffix_item(const AttnArgs& a, int index) 
 // (slots 0-7 or 8-15 of its pages); one or two tiles belong to all waves, a quarter of the tokens each.  The waves' parts
 // are then added through the ring's LDS.  (All waves with the same tokens: 145 us instead of @@ for 32 prefixes of 8192 tokens for 32 rows
 // each, 8 KV heads.)
+//   A row's reference maximum moves only when a lane's weights of a step sum to more than kMaxWeight (none exceeds a sum that passes, and their
+// rounding to bf16 is relative): in the first step and hardly ever after.
 //   Blocks of up to 256 rows (kHalves): half of the tiles each for two workgroups that run on the same XCD, as in attn_kernels.hip; their
-// keys and values are ordinary cached loads, a row's reference maximum moves only when a lane's eight weights sum to more than kMaxWeight.
+// keys and values are ordinary cached loads.
 //   LDS: keys as 64 token rows of 128 bytes, the 16-byte chunk index XOR-ed with bits 1, 4, 5 of the row (the 16 rows of an operand read differ
 // in bits 0, 1, 4, 5, and two rows span the banks), undone on the source side; values as [page][channel][16 slots].
 // ---------------------------------------------------------------------------------------
 constexpr int kStages = 4;
 constexpr int kStepBytes = 2 * kStepPages * kCodeBytes;
+constexpr int kRingSteps = 256;   // whose page ids are there: all of an item's but where a caller names chunks of more than 16128 tokens
 constexpr float kMaxWeight = 256.0f;
 constexpr int waitcnt_imm(int vm, int lgkm) { return (vm & 0xf) | ((vm >> 4) << 14) | (7 << 4) | ((lgkm & 0xf) << 8); }
 struct RingLds {
   __attribute__((aligned(16))) char buf[kStages][kStepBytes];
   __attribute__((aligned(16))) char exponents[kStages][NW][kStepPages * kExponentBytes];   // one copy a wave
+  __attribute__((aligned(16))) int pages[kRingSteps * kStepPages];                         // of steps n at n modulo kRingSteps
 };
 typedef const char __attribute__((address_space(1))) * GlobalBytes;
 typedef char __attribute__((address_space(3))) * LdsBytes;
@@ -174,13 +178,25 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
   const int32_t* table_row = a.prefix_table + (size_t)g * a.max_pp;
   const int nsteps = (tok_end - tok_begin + kStepTok - 1) / kStepTok;
   const int first_page = tok_begin >> 4, last_page = (tok_end - 1) >> 4;
-  // Page ids (scalar) are fetched an iteration before they are used.  A slot past the end repeats the last page: valid bytes that
-  // nobody uses, so that every wait knows how many loads are in flight.
-  uint32_t id_max = 0;
+  // Page ids.  Those of the first steps are read by scalar loads, so that their data is requested at once; all of them go to LDS, checked, from
+  // where a step's are read an iteration before they are used (a scalar load in the loop would be waited for with the next LDS read, and both
+  // are slower than that).  A slot past the end repeats the last page: valid bytes that nobody uses, so that every wait knows how many loads are
+  // in flight.
+  const int n_pages = last_page - first_page + 1;
+  auto checked = [&](int page) {
+    if ((unsigned)page >= (unsigned)a.num_pages) { page = 0; bad_page = 1; }
+    return page;
+  };
   int r[kStepPages];
   auto fetch_ids = [&](int n) {
 #pragma unroll
-    for (int u = 0; u < kStepPages; ++u) r[u] = ld_uniform(table_row + min(first_page + kStepPages * n + u, last_page));
+    for (int u = 0; u < kStepPages; ++u) r[u] = checked(ld_uniform(table_row + min(first_page + kStepPages * n + u, last_page)));
+  };
+  auto read_ids = [&](int n) {
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    const i32x4 v = *reinterpret_cast<const i32x4*>(ring_lds.pages + kStepPages * (n & (kRingSteps - 1)));
+#pragma unroll
+    for (int u = 0; u < kStepPages; ++u) r[u] = __builtin_amdgcn_readfirstlane(v[u]);
   };
   // A step is 1024 16-byte vectors: keys of pages 0 and 1, of 2 and 3, values likewise; a load of a wave is half a page.
   uint32_t src_off[4];
@@ -193,11 +209,7 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
   auto issue = [&](uint32_t ring) {
     uint64_t off[kStepPages];
 #pragma unroll
-    for (int u = 0; u < kStepPages; ++u) {
-      id_max = max(id_max, (uint32_t)r[u]);
-      const uint32_t page = (uint32_t)r[u] < (uint32_t)a.num_pages ? r[u] : 0;
-      off[u] = ((uint64_t)page * (uint32_t)a.Hkv + (uint32_t)kvh) * kCodeBytes;
-    }
+    for (int u = 0; u < kStepPages; ++u) off[u] = ((uint64_t)(uint32_t)r[u] * (uint32_t)a.Hkv + (uint32_t)kvh) * kCodeBytes;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const uint64_t page_off = wave >> 1 ? off[2 * (k & 1) + 1] : off[2 * (k & 1)];
@@ -227,7 +239,11 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
     fetch_ids(s0);
     issue(s0 * kStepBytes);
   }
-  fetch_ids(kStages - 1);
+  auto store_ids = [&](int from, int to) {   // of steps from .. to - 1
+    for (int u = from * kStepPages + tid; u < to * kStepPages; u += NW * 64)
+      ring_lds.pages[u & (kRingSteps * kStepPages - 1)] = checked(table_row[first_page + min(u, n_pages - 1)]);
+  };
+  store_ids(0, min(nsteps + kStages, kRingSteps));
 
   const float sc = scale_of(a);
   const uint32_t sign_flip = sign_flip_of(a);
@@ -253,12 +269,12 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
 
   const uint32_t k_rd = (16 * (i >> 2) + (i & 3)) * kD;
   const uint32_t v_rd = kStepPages * kCodeBytes + kCodeBytes * j + kPage * i;
-  auto run = [&](auto nt_tag) {
-    constexpr int NTraw = decltype(nt_tag)::value;
+  auto run = [&](auto nt_tag, auto sharers_tag) {
+    constexpr int NTraw = decltype(nt_tag)::value, kSharers = decltype(sharers_tag)::value;
     constexpr int NT = NTraw > 0 ? NTraw : 1;   // (no zero-length arrays; a wave without tiles only moves data)
+    constexpr int kTiles = kSharers == 4 ? 1 : 2;
     // 16 kTiles tokens: slots `slot0` .. of the step's pages; `left` tokens of the step exist
-    auto take = [&](auto tiles_tag, uint32_t ring, int slot0, int left) {
-      constexpr int kTiles = decltype(tiles_tag)::value;
+    auto take = [&](uint32_t ring, int slot0, int left) {
       const char* ex = ring_lds.exponents[0][0] + (ring / kStepBytes * NW + wave) * (kStepPages * kExponentBytes) + slot0;
       const char* buf = ring_lds.buf[0] + ring;
       u32x4 kr[kTiles][2];
@@ -316,26 +332,16 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
             psum += (p[4 * T] + p[4 * T + 1]) + (p[4 * T + 2] + p[4 * T + 3]);
           }
         };
-        auto move_reference = [&] {
+        weights();
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(psum > kMaxWeight) != 0, 0)) {   // wave-uniform
           float mx = max4(s[qt][0]);
           if constexpr (kTiles == 2) mx = fmaxf(mx, max4(s[qt][1]));
           const float m_new = fmaxf(t.m, rows_allreduce_max(mx) * sc);
-          if (kHalves || __builtin_amdgcn_ballot_w64(m_new > t.m) != 0) {   // wave-uniform
-            const float alpha = __builtin_amdgcn_exp2f(t.m - m_new);        // 1 where the row did not move
-            t.l *= alpha;
-            t.m = m_new;
+          const float alpha = __builtin_amdgcn_exp2f(t.m - m_new);        // 1 where the row did not move
+          t.l *= alpha;
+          t.m = m_new;
 #pragma unroll
-            for (int ct = 0; ct < 8; ++ct) t.acc[ct] *= alpha;
-          }
-        };
-        if constexpr (kHalves) {
-          weights();
-          if (__builtin_amdgcn_ballot_w64(psum > kMaxWeight) != 0) {   // wave-uniform
-            move_reference();
-            weights();
-          }
-        } else {
-          move_reference();
+          for (int ct = 0; ct < 8; ++ct) t.acc[ct] *= alpha;
           weights();
         }
         t.l += psum;
@@ -359,8 +365,11 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
         for (int qt = 0; qt < NT; ++qt) tile[qt].acc[ct] = mfma_16x16x32(v, w[qt], tile[qt].acc[ct]);
       }
     };
-    constexpr std::integral_constant<int, 1> kQuarter{};
-    constexpr std::integral_constant<int, 2> kHalf{};
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(waitcnt_imm(63, 0));              // this wave's page ids are in LDS
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read_ids(kStages - 1);
     uint32_t ring = 0;
 #pragma unroll 1
     for (int n = 0; n < nsteps; ++n) {
@@ -368,26 +377,36 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_barrier();                              // ... for every wave; all have read slot n - 1
       asm volatile("" ::: "memory");
+      if ((n & (kRingSteps / 2 - 1)) == 0 && n > 0) store_ids(n + kRingSteps / 2, min(nsteps + kStages, n + kRingSteps));
       issue((ring + 3 * kStepBytes) & (kRingBytes - 1));
-      fetch_ids(n + 4);
+      read_ids(n + kStages);
       if constexpr (NTraw > 0) {
         const int left = tok_end - tok_begin - n * kStepTok;
-        if (sharers == 1) {                                      // workgroup-uniform
+        if constexpr (kSharers == 1) {
 #pragma unroll 1
-          for (int h = 0; h < 2; ++h) take(kHalf, ring, 8 * h, left);
-        } else if (sharers == 2) {
-          take(kHalf, ring, 8 * (wave >> 1), left);
+          for (int h = 0; h < 2; ++h) take(ring, 8 * h, left);
         } else {
-          take(kQuarter, ring, 4 * wave, left);
+          take(ring, kSharers == 2 ? 8 * (wave >> 1) : 4 * wave, left);
         }
       }
       ring = (ring + kStepBytes) & (kRingBytes - 1);
     }
   };
-  if (nt == 2) run(std::integral_constant<int, 2>{});
-  else if (nt == 1) run(std::integral_constant<int, 1>{});
-  else run(std::integral_constant<int, 0>{});
-  if (id_max >= (uint32_t)a.num_pages) bad_page = 1;
+  constexpr std::integral_constant<int, 0> k0{};
+  constexpr std::integral_constant<int, 1> k1{};
+  constexpr std::integral_constant<int, 2> k2{};
+  constexpr std::integral_constant<int, 4> k4{};
+  if (sharers == 1) {   // workgroup-uniform; the wave's number of tiles is wave-uniform
+    if (nt == 2) run(k2, k1);
+    else if (nt == 1) run(k1, k1);
+    else run(k0, k1);
+  } else if (sharers == 2) {
+    if (nt == 2) run(k2, k2);
+    else run(k1, k2);
+  } else {
+    if (nt == 2) run(k2, k4);
+    else run(k1, k4);
+  }
 
   const int tid2 = thread_index(), i2 = tid2 & 15, j2 = (tid2 & 63) >> 4;
   if (sharers == 1) {   // workgroup-uniform
