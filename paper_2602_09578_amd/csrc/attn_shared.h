@@ -8,8 +8,6 @@
 namespace marl {
 
 constexpr int kAccRowFloats = kD + 4;   // of a row in LDS (the 16 rows that a wave instruction writes start in different banks)
-constexpr int kMaximaAtOnce = 8;        // of partials that are about to be added
-constexpr int kEager = 4;               // partials of a row that are requested before the first is used
 constexpr int kSeqBlock = 8;            // sequences whose workgroups for one KV head and part run on one XCD
 
 // Four channels of a final row.
@@ -19,71 +17,6 @@ __device__ __forceinline__ void store_row_piece(const AttnArgs& a, size_t at, f3
     *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = v;
   } else {
     *reinterpret_cast<bf16x4*>(reinterpret_cast<uint16_t*>(a.out) + at) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-  }
-}
-
-// Adds the partials of one row, those of npc prefix chunks and nsc own ones, in slot order, and stores the row; half a wave a row.
-__device__ __forceinline__ void merge_row(const AttnArgs& a, const int row, const int npc, const int nsc) {
-  const int sub = threadIdx.x & 31;   // lane within the half wave: channels 4*sub .. 4*sub+3
-  const int n = npc + nsc;
-  const int nslot = a.NCp + a.NCs;
-  const float2* ml = a.partial_ml + (size_t)row * nslot;
-  const float* po = a.partial_o + (size_t)row * nslot * kD + 4 * sub;
-  auto slot_of = [&](int k) { return k < npc ? k : a.NCp + (k - npc); };
-
-  float2 mlk[kEager];
-  f32x4 ok[kEager];
-#pragma unroll
-  for (int k = 0; k < kEager; ++k) {
-    mlk[k] = make_float2(-INFINITY, 0.f);
-    ok[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (k < n) {
-      const int sl = slot_of(k);
-      mlk[k] = ml[sl];
-      ok[k] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(po + (size_t)sl * kD));
-    }
-  }
-  float mstar = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < kEager; ++k) mstar = fmaxf(mstar, mlk[k].x);
-  for (int k = kEager; k < n; k += kMaximaAtOnce) {
-    float mk[kMaximaAtOnce];
-#pragma unroll
-    for (int u = 0; u < kMaximaAtOnce; ++u) mk[u] = ml[slot_of(min(k + u, n - 1))].x;
-#pragma unroll
-    for (int u = 0; u < kMaximaAtOnce; ++u) mstar = fmaxf(mstar, mk[u]);
-  }
-
-  float denom = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int k = 0; k < kEager; ++k) {
-    const float f = (mlk[k].x == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(mlk[k].x - mstar);
-    denom = __builtin_fmaf(mlk[k].y, f, denom);
-    acc += ok[k] * f;
-  }
-  for (int k = kEager; k < n; k += kEager) {   // as many at once as before the first use
-#pragma unroll
-    for (int u = 0; u < kEager; ++u) {
-      const int sl = slot_of(min(k + u, n - 1));
-      mlk[u] = ml[sl];
-      ok[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(po + (size_t)sl * kD));
-    }
-#pragma unroll
-    for (int u = 0; u < kEager; ++u) {
-      const float f = (mlk[u].x == -INFINITY || k + u >= n) ? 0.f : __builtin_amdgcn_exp2f(mlk[u].x - mstar);
-      denom = __builtin_fmaf(mlk[u].y, f, denom);
-      acc += ok[u] * f;
-    }
-  }
-  f32x4 r = {0.f, 0.f, 0.f, 0.f};
-  if (n > 0 && denom > 0.f) r = acc * (1.0f / denom);
-  if (a.out_dtype == MARL_OUT_F32) {
-    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + (size_t)row * kD + 4 * sub) = r;
-  } else {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    const bf16x4 v = {(__bf16)r[0], (__bf16)r[1], (__bf16)r[2], (__bf16)r[3]};
-    *reinterpret_cast<bf16x4*>(reinterpret_cast<uint16_t*>(a.out) + (size_t)row * kD + 4 * sub) = v;
   }
 }
 
