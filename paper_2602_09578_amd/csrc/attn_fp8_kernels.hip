@@ -766,14 +766,14 @@ constexpr int kRowsPerBlock = kAttnThreads / 32;
 __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void merge_fp8_kernel(AttnArgs a) {
   const int row = blockIdx.x * kRowsPerBlock + (threadIdx.x >> 5);
-  const bool there = row < a.NS * a.Hq;
-  const int info = there ? a.seq_chunks[row / a.Hq] : 0x10000;
-  const int own = there ? min(a.suffix_lens[row / a.Hq], a.max_sp * kPage) : 0;
+  const int rows = a.NS * a.Hq, seq = min(row, rows - 1) / a.Hq;   // (loads without a branch, which would be waited for before the items)
+  const int info = a.seq_chunks[seq];
+  const int own = min(a.suffix_lens[seq], a.max_sp * kPage);
   int bad_page = 0;
   short_suffix_items<true>(a, bad_page);
   if (bad_page) atomicOr(&a.counters[MARL_CTR_FLAGS], MARL_FLAG_BAD_PAGE);
   const int npc = info & 0xffff, nsc = info >> 16;
-  if (nsc == 1 && (npc == 0 || own <= kShortTokens)) return;   // finished above, or in the items kernel
+  if (row >= rows || (nsc == 1 && (npc == 0 || own <= kShortTokens))) return;   // finished above, or in the items kernel
   merge_row(a, row, npc, nsc);
 }
 
