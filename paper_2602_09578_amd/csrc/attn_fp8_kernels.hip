@@ -5,6 +5,10 @@
 //
 // With half the bytes per token the fixed costs of an item weigh twice as much as over a bf16 cache, and the vector ALU has codes to
 // convert: so items follow each other without a gap, and waves without a row tile of their own share the others' tokens.
+//   Measured (a call; kernels in order plan, items, merge): 128 sequences of 8192 to 24576 own tokens and 32 prefixes of 8192, 64 / 8 heads,
+// 4932 MB: 795 us (7, 782, 10; 6.3 TB/s in the items kernel, where the loads alone reach 6.8 and a plain read 7.0).  512 of a median of 256 to
+// 2048 (at most 8192) and 64 prefixes of 512 to 2048, 28 / 4 heads, 789 MB: 182 us (6, 162, 12): the longest item, one workgroup's share of the
+// memory's rate, ends last.
 #include <algorithm>
 #include <type_traits>
 
@@ -101,6 +105,8 @@ __device__ __forceinline__ void store_partial(const AttnArgs& a, size_t slot, in
 //   The next item is known while this one runs (see the queue below): its record and page ids are fetched while a wave waits for its last
 // step's data, and its first keys, queries and values are requested where the last step frees the registers, so that they are under way
 // while the waves' results are added.
+//   What bounds them: memory, 6.3 TB/s.  A step's registers are its only look-ahead (186 of the 256 that two waves of a SIMD have), which is
+// as many bytes as the memory needs: the same items on pages that the caches hold take half the time.
 // ---------------------------------------------------------------------------------------
 struct SuffixItem {
   const int32_t* row;   // of the block table
@@ -125,12 +131,16 @@ __device__ __forceinline__ SuffixItem suffix_item(const AttnArgs& a, int index) 
 //   A block has up to eight row tiles of 16.  With five to eight, tile t belongs to wave t % 4, which takes all tokens.  With fewer, waves would idle or
 // convert all codes for a single tile: three or four tiles are taken in pairs, and the two waves of a pair take half of each step's tokens
 // (slots 0-7 or 8-15 of its pages); one or two tiles belong to all waves, a quarter of the tokens each.  The waves' parts
-// are then added through the ring's LDS.  (All waves with the same tokens: 145 us instead of @@ for 32 prefixes of 8192 tokens for 32 rows
-// each, 8 KV heads.)
+// are then added through the ring's LDS.  (All waves with the same tokens: 145 us instead of 110 for a call over 32 prefixes of 8192 tokens
+// for 32 rows each, 8 KV heads.)
 //   A row's reference maximum moves only when a lane's weights of a step sum to more than kMaxWeight (none exceeds a sum that passes, and their
 // rounding to bf16 is relative): in the first step and hardly ever after.
 //   Blocks of up to 256 rows (kHalves): half of the tiles each for two workgroups that run on the same XCD, as in attn_kernels.hip; their
 // keys and values are ordinary cached loads.
+//   What bounds them: the issue of instructions.  A step of a wave with two tiles is about 480 of them and 64 matrix instructions; the two
+// waves of a SIMD take 2.4 us for theirs.  16 prefixes of 4096 tokens for 224 rows, 4 KV heads, 30 GFLOP: 61 us in the items kernel (0.49 PFLOP/s),
+// the same on pages that the caches hold.  Measured and left out: scores by products of 8-bit numbers (the queries as two of them each, 74 to
+// 77 us a call instead of 76), one half of a step's weights beside the other half's scores (79), chunks of twice the default (88).
 //   LDS: keys as 64 token rows of 128 bytes, the 16-byte chunk index XOR-ed with bits 1, 4, 5 of the row (the 16 rows of an operand read differ
 // in bits 0, 1, 4, 5, and two rows span the banks), undone on the source side; values as [page][channel][16 slots].
 // ---------------------------------------------------------------------------------------
@@ -702,7 +712,6 @@ void items_fp8_kernel(AttnArgs a) { items_kernel_body<false>(a); }
 __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void items_fp8_kernel_wide(AttnArgs a) { items_kernel_body<true>(a); }
 
-// Merge kernel: first the sequences whose own tokens are one short item, then the other rows' partials, half a wave a row.
 // Adds the partials of one row, those of npc prefix chunks and nsc own ones, in slot order, and stores the row; half a wave a row.
 __device__ __forceinline__ void merge_row(const AttnArgs& a, const int row, const int npc, const int nsc) {
   const int sub = threadIdx.x & 31;   // lane within the half wave: channels 4*sub .. 4*sub+3
@@ -762,6 +771,10 @@ __device__ __forceinline__ void merge_row(const AttnArgs& a, const int row, cons
   store_row_piece(a, (size_t)row * kD + 4 * sub, r);
 }
 
+// Merge kernel: first the sequences whose own tokens are one short item, then the other rows' partials, half a wave a row.
+// What bounds it: chains of dependent loads (the lists' lengths, an item, its page ids, its keys, the prefix partials).  10 us for 8192 rows of up
+// to five partials, 12 for 14336 of up to three, 15 for 2048 items of up to 64 tokens with four prefix partials each.  Two to four rows for half a wave
+// at once were 1 to 3 us slower.
 constexpr int kRowsPerBlock = kAttnThreads / 32;
 __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void merge_fp8_kernel(AttnArgs a) {
@@ -779,6 +792,8 @@ void merge_fp8_kernel(AttnArgs a) {
 
 // ---------------------------------------------------------------------------------------
 // A small call: one workgroup takes the tokens, prefix and own, of one part of a (sequence, KV head), as in attn_small_kernel.hip.
+//   What bounds it: one chain of loads (lengths, page ids, keys, values) and the launch.  16 sequences of 4 prompts of 256 tokens and up to 128 of
+// their own, 8 / 2 heads: 6 us.
 // ---------------------------------------------------------------------------------------
 __device__ __forceinline__ void small_item(const AttnArgs& a, const int s, const int kvh, const int part) {
   __shared__ TileLds lds;
