@@ -146,13 +146,13 @@ __device__ __forceinline__ SuffixItem suffix_item(const AttnArgs& a, int index) 
 // ---------------------------------------------------------------------------------------
 constexpr int kStages = 4;
 constexpr int kStepBytes = 2 * kStepPages * kCodeBytes;
-constexpr int kRingSteps = 256;   // whose page ids are there: all of an item's but where a caller names chunks of more than 16128 tokens
+constexpr int kRingSteps = 256;   // whose block numbers are there: all of an item's but where a caller names chunks of more than 16128 tokens
 constexpr float kMaxWeight = 256.0f;
 constexpr int waitcnt_imm(int vm, int lgkm) { return (vm & 0xf) | ((vm >> 4) << 14) | (7 << 4) | ((lgkm & 0xf) << 8); }
 struct RingLds {
   __attribute__((aligned(16))) char buf[kStages][kStepBytes];
   __attribute__((aligned(16))) char exponents[kStages][NW][kStepPages * kExponentBytes];   // one copy a wave
-  __attribute__((aligned(16))) int pages[kRingSteps * kStepPages];                         // of steps n at n modulo kRingSteps
+  __attribute__((aligned(16))) uint32_t blocks[kRingSteps * kStepPages];                   // of steps n at n modulo kRingSteps
 };
 typedef const char __attribute__((address_space(1))) * GlobalBytes;
 typedef char __attribute__((address_space(3))) * LdsBytes;
@@ -190,25 +190,23 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
   const int32_t* table_row = a.prefix_table + (size_t)g * a.max_pp;
   const int nsteps = (tok_end - tok_begin + kStepTok - 1) / kStepTok;
   const int first_page = tok_begin >> 4, last_page = (tok_end - 1) >> 4;
-  // Page ids.  Those of the first steps are read by scalar loads, so that their data is requested at once; all of them go to LDS, checked, from
-  // where a step's are read an iteration before they are used (a scalar load in the loop would be waited for with the next LDS read, and both
-  // are slower than that).  A slot past the end repeats the last page: valid bytes that nobody uses, so that every wait knows how many loads are
-  // in flight.
+  // A block is a page's keys or values of one KV head; its number is that of its exponents too.  Numbers of the first steps come straight from
+  // the block table, so that their data is requested at once; all of them go to LDS, checked, from where a step's are read an iteration before
+  // they are used (a scalar load in the loop would be waited for with the next LDS read, and both are slower than that).  A slot past the end
+  // repeats the last page: valid bytes that nobody uses, so that every wait knows how many loads are in flight.
   const int n_pages = last_page - first_page + 1;
-  auto checked = [&](int page) {
+  auto block_of = [&](int page) {
     if ((unsigned)page >= (unsigned)a.num_pages) { page = 0; bad_page = 1; }
-    return page;
+    return (uint32_t)page * (uint32_t)a.Hkv + (uint32_t)kvh;
   };
-  int r[kStepPages];
-  auto fetch_ids = [&](int n) {
-#pragma unroll
-    for (int u = 0; u < kStepPages; ++u) r[u] = checked(ld_uniform(table_row + min(first_page + kStepPages * n + u, last_page)));
+  // what a wave takes of a step: the two blocks of its loads, and the one whose exponents the lane asks for
+  struct Blocks {
+    uint32_t b0, b1, mine;
   };
-  auto read_ids = [&](int n) {
-    typedef int i32x4 __attribute__((ext_vector_type(4)));
-    const i32x4 v = *reinterpret_cast<const i32x4*>(ring_lds.pages + kStepPages * (n & (kRingSteps - 1)));
-#pragma unroll
-    for (int u = 0; u < kStepPages; ++u) r[u] = __builtin_amdgcn_readfirstlane(v[u]);
+  const int half_step = wave >> 1, mine_at = (lane >> 1) & (kStepPages - 1);
+  auto read_blocks = [&](int n) {
+    const uint32_t* p = ring_lds.blocks + kStepPages * (n & (kRingSteps - 1));
+    return Blocks{(uint32_t)__builtin_amdgcn_readfirstlane(p[half_step]), (uint32_t)__builtin_amdgcn_readfirstlane(p[2 + half_step]), p[mine_at]};
   };
   // A step is 1024 16-byte vectors: keys of pages 0 and 1, of 2 and 3, values likewise; a load of a wave is half a page.
   uint32_t src_off[4];
@@ -218,14 +216,11 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
     const int key = ((pos >> 4) & 1) | (wave >> 1) << 1 | (k & 1) << 2;
     src_off[k] = 16u * (uint32_t)((k >> 1) ? pos : pos ^ key);
   }
-  auto issue = [&](uint32_t ring) {
-    uint64_t off[kStepPages];
-#pragma unroll
-    for (int u = 0; u < kStepPages; ++u) off[u] = ((uint64_t)(uint32_t)r[u] * (uint32_t)a.Hkv + (uint32_t)kvh) * kCodeBytes;
+  auto issue = [&](uint32_t ring, const Blocks& blocks) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const uint64_t page_off = wave >> 1 ? off[2 * (k & 1) + 1] : off[2 * (k & 1)];
-      const GlobalBytes base = reinterpret_cast<GlobalBytes>(reinterpret_cast<uintptr_t>((k >> 1) ? a.v_pages : a.k_pages)) + page_off;
+      const GlobalBytes base = reinterpret_cast<GlobalBytes>(reinterpret_cast<uintptr_t>((k >> 1) ? a.v_pages : a.k_pages)) +
+                               (uint64_t)(k & 1 ? blocks.b1 : blocks.b0) * kCodeBytes;
       char* dst = ring_lds.buf[0] + (ring + k * 4096 + wave * 1024);   // wave-uniform; lane l lands at dst + 16 l
       uint32_t at = src_off[k];
       asm volatile("" : "+v"(at));   // (an offset to a scalar base, not four 64-bit addresses kept for all steps)
@@ -234,9 +229,8 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
           reinterpret_cast<__attribute__((address_space(3))) void*>((uint32_t)reinterpret_cast<uintptr_t>(dst)), 16, 0, kHalves ? 0 : 2);   // (2: non-temporal)
     }
     if (lane < 2 * kStepPages) {   // lane 2 u + x: the exponents of page u, keys (x = 0) or values
-      const uint64_t page_off = lane < 4 ? (lane < 2 ? off[0] : off[1]) : (lane < 6 ? off[2] : off[3]);
       const GlobalBytes src = reinterpret_cast<GlobalBytes>(reinterpret_cast<uintptr_t>(a.exponents)) +
-                              page_off / (kCodeBytes / kExponentBytes) + (lane & 1) * kPage;
+                              (uint64_t)blocks.mine * kExponentBytes + (lane & 1) * kPage;
       char* dst = ring_lds.exponents[0][0] + (ring / kStepBytes * NW + wave) * (kStepPages * kExponentBytes);
       __builtin_amdgcn_global_load_lds(
           reinterpret_cast<const __attribute__((address_space(1))) void*>(src),
@@ -246,16 +240,21 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
   constexpr uint32_t kRingBytes = kStages * kStepBytes;
   static_assert((kRingBytes & (kRingBytes - 1)) == 0, "the ring wraps by a mask");
   // the first three steps are requested before the chain of dependent loads that leads to the query rows
+  int page0[kStages - 1], page1[kStages - 1], page_mine[kStages - 1];
 #pragma unroll
   for (int s0 = 0; s0 < kStages - 1; ++s0) {
-    fetch_ids(s0);
-    issue(s0 * kStepBytes);
+    const int page = first_page + kStepPages * s0;
+    page0[s0] = ld_uniform(table_row + min(page + half_step, last_page));
+    page1[s0] = ld_uniform(table_row + min(page + 2 + half_step, last_page));
+    page_mine[s0] = table_row[min(page + mine_at, last_page)];
   }
-  auto store_ids = [&](int from, int to) {   // of steps from .. to - 1
+#pragma unroll
+  for (int s0 = 0; s0 < kStages - 1; ++s0) issue(s0 * kStepBytes, Blocks{block_of(page0[s0]), block_of(page1[s0]), block_of(page_mine[s0])});
+  auto store_blocks = [&](int from, int to) {   // of steps from .. to - 1
     for (int u = from * kStepPages + tid; u < to * kStepPages; u += NW * 64)
-      ring_lds.pages[u & (kRingSteps * kStepPages - 1)] = checked(table_row[first_page + min(u, n_pages - 1)]);
+      ring_lds.blocks[u & (kRingSteps * kStepPages - 1)] = block_of(table_row[first_page + min(u, n_pages - 1)]);
   };
-  store_ids(0, min(nsteps + kStages, kRingSteps));
+  store_blocks(0, min(nsteps + kStages, kRingSteps));
 
   const float sc = scale_of(a);
   const uint32_t sign_flip = sign_flip_of(a);
@@ -289,19 +288,17 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
     auto take = [&](uint32_t ring, int slot0, int left) {
       const char* ex = ring_lds.exponents[0][0] + (ring / kStepBytes * NW + wave) * (kStepPages * kExponentBytes) + slot0;
       const char* buf = ring_lds.buf[0] + ring;
+      typedef uint32_t Words __attribute__((ext_vector_type(kTiles)));   // (a word is four slots)
       u32x4 kr[kTiles][2];
-      uint32_t kx[kTiles], vx[kTiles], vr[8][kTiles];   // a word is four slots
+      Words vr[8];
+      const Words kx = *reinterpret_cast<const Words*>(ex + (i >> 2) * kExponentBytes);
+      const Words vx = *reinterpret_cast<const Words*>(ex + j * kExponentBytes + kPage);
 #pragma unroll
-      for (int T = 0; T < kTiles; ++T) {
-        kx[T] = *reinterpret_cast<const uint32_t*>(ex + (i >> 2) * kExponentBytes + 4 * T);
+      for (int T = 0; T < kTiles; ++T)
 #pragma unroll
         for (int c = 0; c < 2; ++c) kr[T][c] = *reinterpret_cast<const u32x4*>(buf + k_rd + (slot0 + 4 * T) * kD + (((4 * c + j) ^ (i >> 1)) << 4));
-        vx[T] = *reinterpret_cast<const uint32_t*>(ex + j * kExponentBytes + kPage + 4 * T);
-      }
 #pragma unroll
-      for (int ct = 0; ct < 8; ++ct)
-#pragma unroll
-        for (int T = 0; T < kTiles; ++T) vr[ct][T] = *reinterpret_cast<const uint32_t*>(buf + v_rd + slot0 + ct * (16 * kPage) + 4 * T);
+      for (int ct = 0; ct < 8; ++ct) vr[ct] = *reinterpret_cast<const Words*>(buf + v_rd + slot0 + ct * (16 * kPage));
       f32x4 s[NT][kTiles];
 #pragma unroll
       for (int T = 0; T < kTiles; ++T) {
@@ -378,10 +375,10 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
       }
     };
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(waitcnt_imm(63, 0));              // this wave's page ids are in LDS
+    __builtin_amdgcn_s_waitcnt(waitcnt_imm(63, 0));              // this wave's block numbers are in LDS
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    read_ids(kStages - 1);
+    Blocks next = read_blocks(kStages - 1);
     uint32_t ring = 0;
 #pragma unroll 1
     for (int n = 0; n < nsteps; ++n) {
@@ -389,9 +386,9 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_barrier();                              // ... for every wave; all have read slot n - 1
       asm volatile("" ::: "memory");
-      if ((n & (kRingSteps / 2 - 1)) == 0 && n > 0) store_ids(n + kRingSteps / 2, min(nsteps + kStages, n + kRingSteps));
-      issue((ring + 3 * kStepBytes) & (kRingBytes - 1));
-      read_ids(n + kStages);
+      if ((n & (kRingSteps / 2 - 1)) == 0 && n > 0) store_blocks(n + kRingSteps / 2, min(nsteps + kStages, n + kRingSteps));
+      issue((ring + 3 * kStepBytes) & (kRingBytes - 1), next);
+      next = read_blocks(n + kStages);
       if constexpr (NTraw > 0) {
         const int left = tok_end - tok_begin - n * kStepTok;
         if constexpr (kSharers == 1) {
