@@ -5,8 +5,8 @@
 //
 // With half the bytes per token the fixed costs of an item weigh twice as much as over a bf16 cache, and the vector ALU has codes to
 // convert: so items follow each other without a gap, and waves without a row tile of their own share the others' tokens.
-//   Measured (a call; kernels in order plan, items, merge): 128 sequences of 8192 to 24576 own tokens and 32 prefixes of 8192, 64 / 8 heads,
-// 4932 MB: 795 us (7, 782, 10; 6.3 TB/s in the items kernel, where the loads alone reach 6.8 and a plain read 7.0).  512 of a median of 256 to
+//   Measured (a call; its plan, items and merge kernels): 128 sequences of 8192 to 24576 own tokens and 32 prefixes of 8192, 64 / 8 heads,
+// 4932 MB: 796 us (7, 781, 12; 6.3 TB/s in the items kernel, where the loads alone reach 6.8 and a plain read 7.0).  512 of a median of 256 to
 // 2048 (at most 8192) and 64 prefixes of 512 to 2048, 28 / 4 heads, 789 MB: 182 us (6, 162, 12): the longest item, one workgroup's share of the
 // memory's rate, ends last.
 #include <algorithm>
@@ -137,10 +137,10 @@ __device__ __forceinline__ SuffixItem suffix_item(const AttnArgs& a, int index) 
 // rounding to bf16 is relative): in the first step and hardly ever after.
 //   Blocks of up to 256 rows (kHalves): half of the tiles each for two workgroups that run on the same XCD, as in attn_kernels.hip; their
 // keys and values are ordinary cached loads.
-//   What bounds them: the issue of instructions.  A step of a wave with two tiles is about 480 of them and 64 matrix instructions; the two
-// waves of a SIMD take 2.4 us for theirs.  16 prefixes of 4096 tokens for 224 rows, 4 KV heads, 30 GFLOP: 61 us in the items kernel (0.49 PFLOP/s),
-// the same on pages that the caches hold.  Measured and left out: scores by products of 8-bit numbers (the queries as two of them each, 74 to
-// 77 us a call instead of 76), one half of a step's weights beside the other half's scores (79), chunks of twice the default (88).
+//   What bounds them: the issue of instructions.  A step of a wave with two tiles is about 560 of them, 64 of these matrix instructions.  16 prefixes
+// of 4096 tokens for 224 rows, 4 KV heads, 30 GFLOP: 56 us in the items kernel (0.54 PFLOP/s), the same on pages that the caches hold.  Measured
+// and left out: scores by products of 8-bit numbers (the queries as two of them each: 71 us a call instead of 74, but calls bound by memory
+// 0.5 to 1 % slower), one half of a step's weights beside the other half's scores (3 % slower), chunks of twice the default (88 us).
 //   LDS: keys as 64 token rows of 128 bytes, the 16-byte chunk index XOR-ed with bits 1, 4, 5 of the row (the 16 rows of an operand read differ
 // in bits 0, 1, 4, 5, and two rows span the banks), undone on the source side; values as [page][channel][16 slots].
 // ---------------------------------------------------------------------------------------
@@ -392,7 +392,7 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
       if constexpr (NTraw > 0) {
         const int left = tok_end - tok_begin - n * kStepTok;
         if constexpr (kSharers == 1) {
-#pragma unroll 1
+#pragma unroll
           for (int h = 0; h < 2; ++h) take(ring, 8 * h, left);
         } else {
           take(ring, kSharers == 2 ? 8 * (wave >> 1) : 4 * wave, left);
@@ -769,8 +769,8 @@ __device__ __forceinline__ void merge_row(const AttnArgs& a, const int row, cons
 }
 
 // Merge kernel: first the sequences whose own tokens are one short item, then the other rows' partials, half a wave a row.
-// What bounds it: chains of dependent loads (the lists' lengths, an item, its page ids, its keys, the prefix partials).  10 us for 8192 rows of up
-// to five partials, 12 for 14336 of up to three, 15 for 2048 items of up to 64 tokens with four prefix partials each.  Two to four rows for half a wave
+// What bounds it: chains of dependent loads (the lists' lengths, an item, its page ids, its keys, the prefix partials).  13 us for 8192 rows of up
+// to five partials, 13 for 14336 of up to three, 15 for 2048 items of up to 64 tokens with four prefix partials each.  Two to four rows for half a wave
 // at once were 1 to 3 us slower.
 constexpr int kRowsPerBlock = kAttnThreads / 32;
 __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
