@@ -368,7 +368,10 @@ int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, con
  * marl_decode_attn_fp8: marl_decode_attn over such a cache: the same operation on the values that the codes stand for, the same shape,
  * workspace (marl_workspace_bytes), work lists, flags and limits; q stays bf16.  A token's row whose exponent lies outside what the writing calls
  * store ([-110, 120]) gives unspecified values, codes and exponents that no token owns are never read into a result.  The weights are
- * rounded to bf16 before they multiply the values, as in marl_decode_attn; everything else is float32.
+ * rounded to bf16 before they multiply the values, as in marl_decode_attn; everything else is float32.  Its items are those of
+ * marl_decode_attn's lists, always taken by one kernel (the event timing counts it as the suffix stage).  Default chunks are the same too:
+ * where few own lengths are near the table rows' end, a caller that names half of a default suffix chunk of 8192 tokens, and makes its
+ * workspace for that, evens out the call's end (512 sequences of 1 to 8192 own tokens: 171 us instead of 179).
  */
 int marl_kv_append_fp8(const marl_attn_shape* shape, const void* k_new, const void* v_new,
                        void* k_pages, void* v_pages, int8_t* exponents, const int32_t* suffix_block_table,

@@ -96,8 +96,10 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_fp8_kernel(KvAppendF
 
 // bf16 page dst[i] <- 8-bit page src[i]: one workgroup per (pair, KV head), a thread for eight codes of the keys and eight of the
 // values, so that a wave stores 1 KB at a time.  The exponents of eight neighbouring slots of a value row are one load.
-// What bounds it: memory.  3001 pages x 8 heads, 296 MB: 45 us (6.6 TB/s) with stores past the caches, 61 through them; what
-// the XCDs' caches (4 MB each) can hold goes through them to whoever reads it next.
+// What bounds it: memory, two thirds of it writes.  3001 pages x 8 heads, 296 MB: 45 us (6.6 TB/s) where the codes are still in the memory's
+// own cache, 55 to 59 where they are not (a large copy reaches the same 5 TB/s); 2 to 16 us more with stores through the caches, and as
+// much with two, four or eight (page, KV head) pairs a workgroup (2, 4, 11).  What the XCDs' caches (4 MB each) can hold goes through them to
+// whoever reads it next.
 constexpr long kReadCacheBytes = 32l << 20;
 template <bool kPastCaches>
 __global__ __launch_bounds__(256) void kv_read_pages_fp8_kernel(KvReadFp8Args a) {

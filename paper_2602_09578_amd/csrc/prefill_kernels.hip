@@ -996,7 +996,8 @@ __device__ __forceinline__ void write_prompt_page_bf16(const PrefillArgs& a, con
 
 // The same into an 8-bit cache (kv_fp8.h).  16 lanes take a row, 8 channels each, so a thread has two pieces of the keys and two of the
 // values; those of a page are quantised first, and the codes of the values turned in LDS: thread c collects channel c's 16 bytes.
-// What bounds it: memory.  64 prompts of 512 to 2048 tokens, 4 KV heads, 270 MB: 51 us (5.2 TB/s); 56 with loads that stay in the caches.
+// What bounds it: memory.  64 prompts of 512 to 2048 tokens, 4 KV heads, 270 MB: 50 us (5.4 TB/s; 56 where
+// nothing of it is in the memory's own cache); 5 us more with loads that stay in the caches.
 struct PromptCodes {
   __attribute__((aligned(8))) uint8_t v[kPage][kD + 8];   // (rows 34 words apart: 16 lanes' pieces of four rows meet in two banks at most)
 };
