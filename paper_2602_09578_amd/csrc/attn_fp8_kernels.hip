@@ -133,7 +133,7 @@ __device__ __forceinline__ SuffixItem suffix_item(const AttnArgs& a, int index) 
 // (slots 0-7 or 8-15 of its pages); one or two tiles belong to all waves, a quarter of the tokens each.  The waves' parts
 // are then added through the ring's LDS.  (All waves with the same tokens: 145 us instead of 110 for a call over 32 prefixes of 8192 tokens
 // for 32 rows each, 8 KV heads.)
-//   A row's reference maximum moves only when a lane's weights of a step sum to more than kMaxWeight (none exceeds a sum that passes, and their
+//   A row's reference maximum moves only when a lane's weights of that row in a step sum to more than kMaxWeight (none exceeds a sum that passes, and their
 // rounding to bf16 is relative): in the first step and hardly ever after.
 //   Blocks of up to 256 rows (kHalves): half of the tiles each for two workgroups that run on the same XCD, as in attn_kernels.hip; their
 // keys and values are ordinary cached loads.
@@ -183,7 +183,10 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
   if (kHalves && tiles <= 0) return;                         // workgroup-uniform (a first half is never empty)
   const int row_begin = it.w + (half ? tiles0 * 16 : 0);
   // the wave's tiles first, first + stride, and its share of the tokens: `sharers` waves have the same tiles
-  const int sharers = tiles <= 2 ? 4 : tiles <= 4 ? 2 : 1;
+  // (the rows of a group of more than 64 sequences lie in the order in which the plan met them: all its blocks add their tokens in the same way,
+  // so that a row's bits do not depend on its place)
+  const bool any_order = nrows > max(64 * a.R, kRowsPerQBlock);
+  const int sharers = any_order ? 1 : tiles <= 2 ? 4 : tiles <= 4 ? 2 : 1;
   const int first_tile = sharers == 4 ? 0 : sharers == 2 ? 2 * (wave & 1) : wave, tile_stride = sharers == 1 ? NW : 1;
   const int nt = sharers == 1 ? (tiles > wave + NW ? 2 : tiles > wave ? 1 : 0) : min(2, tiles - first_tile);
 
@@ -345,7 +348,8 @@ __device__ __forceinline__ void prefix_item(const AttnArgs& a, const int4 it, co
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(psum > kMaxWeight) != 0, 0)) {   // wave-uniform
           float mx = max4(s[qt][0]);
           if constexpr (kTiles == 2) mx = fmaxf(mx, max4(s[qt][1]));
-          const float m_new = fmaxf(t.m, rows_allreduce_max(mx) * sc);
+          // (to the maximum of the row's lanes with such sums: its neighbours in the tile have no say)
+          const float m_new = fmaxf(t.m, rows_allreduce_max(psum > kMaxWeight ? mx : -INFINITY) * sc);
           const float alpha = __builtin_amdgcn_exp2f(t.m - m_new);        // 1 where the row did not move
           t.l *= alpha;
           t.m = m_new;

@@ -150,6 +150,24 @@ def test_many_pairs(seqs, Hkv, samples):
     assert c.stages(suffix_chunk_tokens=512) == {"plan", "suffix", "merge"}
 
 
+@pytest.mark.parametrize("members,alone,Hq,Hkv", [(150, 12, 4, 4), (70, 0, 14, 2), (80, 0, 4, 2), (69, 2, 28, 4)])
+def test_a_row_does_not_depend_on_its_place(members, alone, Hq, Hkv):
+    """Samples of one prompt in another order, in groups larger than the plan puts in order (64): the same bits for each, in blocks of 128 and of 256 rows
+    and in what is left after them."""
+    print("case: fp8 attention, order of rows", members, Hq, flush=True)
+    rng = np.random.default_rng(members)
+    slens = rng.integers(0, 150, members + alone)
+    gos = np.concatenate([np.zeros(members, int), 1 + np.arange(alone)])
+    c = Cache(custom_inputs([777] + [40] * alone, slens, gos, Hq, Hkv, seed=members))
+    chunks = dict(suffix_chunk_tokens=256, prefix_chunk_tokens=256)
+    got, _ = c.run(**chunks)
+    order = torch.from_numpy(rng.permutation(members + alone))
+    d = c.dev
+    c.dev = I.AttnInputs(**{**d.__dict__, **{k: getattr(d, k)[order.cuda()].contiguous() for k in ("q", "suffix_block_table", "suffix_lens", "group_of_seq")}})
+    again, _ = c.run(**chunks)
+    assert np.array_equal(again, got[order.numpy()])
+
+
 @pytest.mark.parametrize("name,pdiv,ldiv", [("tiny", 1, 1), ("qwen7b", 16, 4), ("skew", 8, 8), ("prefix", 16, 4), ("long32b", 8, 8)])
 def test_scaled_workloads(name, pdiv, ldiv):
     print("case: fp8 attention", name, flush=True)
