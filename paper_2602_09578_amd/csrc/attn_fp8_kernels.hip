@@ -581,7 +581,29 @@ __device__ __forceinline__ void short_suffix_items(const AttnArgs& a, int& bad_p
 // items, the other suffix items.  A workgroup's first entry is its index, its second the mirror image of that in the next round (the list is
 // sorted, longest first); it draws the one after the next while it works on one.  A sequence's long suffix item is left as a partial but where
 // the sequence has no prefix and no other item.
+//   Two workgroups a CU ask for more than the memory can bring, and an item gets a 512th of its rate: one that is much longer than the others
+// then ends long after them.  Where the list says so (ends_late), one workgroup a CU, enough to keep the memory busy, takes the suffix items, each
+// at twice the rate, and the other the prefix items, which leave the memory time.  512 sequences of a median of 256 to 2048 tokens, 8192 at most:
+// 182 -> 169 us; 640 with a median of 600: 174 -> 159; 16 x 32 with a median of 512 and 256-row prefix items: 141 -> 128.  Where items are about as long, it would
+// cost 5 % (1024 sequences of 200 to 1000 tokens: 130 -> 137) to 20 (32 x 12 short ones after prefixes of 1000 to 6000: 88 -> 108); asking costs 1 us.
 // ---------------------------------------------------------------------------------------
+// Tokens of an item, as the plan lists them (longest first).
+__device__ __forceinline__ int tokens_of(const int4* item) {
+  const int32_t* rec = reinterpret_cast<const int32_t*>(item);
+  return ld_uniform(rec + 2) - ld_uniform(rec + 1);
+}
+// Whether the longest suffix item, at one workgroup's share of the memory's rate, would end after all others: its tokens against what each of
+// `grid` workgroups takes, the mean by the items in the middle of the list's quarters.
+__device__ __forceinline__ bool ends_late(const AttnArgs& a, int suffix_items, int prefix_items, int grid) {
+  const int longest = tokens_of(a.suffix_items);
+  int four = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) four += tokens_of(a.suffix_items + (int)((2 * k + 1) * (long)suffix_items / 8));
+  const int prefix = prefix_items > 0 ? tokens_of(a.prefix_items + prefix_items / 2) * kPrefixTokenCost : 0;
+  const float all = ((float)suffix_items * (float)four * 0.25f + (float)prefix_items * (float)prefix) * (float)a.Hkv;
+  return (float)longest * (float)grid > all;
+}
+
 template <bool kWide>
 __device__ __forceinline__ void items_kernel_body(const AttnArgs& a) {
   __shared__ ItemLds lds;
@@ -597,7 +619,10 @@ __device__ __forceinline__ void items_kernel_body(const AttnArgs& a) {
   const int grid = gridDim.x;
   const bool as_entries = partials && n_prefix + n_all <= grid + grid / 2;
   const int n_suffix = as_entries ? n_all : n_long;
-  const int head = a.counters[MARL_CTR_NUM_FIRST_SUFFIX_ITEMS] * a.Hkv;
+  // (apart, a streamer has two suffix items at least)
+  const int streamers = (grid + 1) / 2, others = grid - streamers;
+  const bool apart = !as_entries && n_suffix >= 2 * streamers && ends_late(a, n_suffix / a.Hkv, pairs / a.Hkv, grid);
+  const int head = apart ? 0 : a.counters[MARL_CTR_NUM_FIRST_SUFFIX_ITEMS] * a.Hkv;
   const int total = n_prefix + n_suffix;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float sc = scale_of(a);
@@ -619,13 +644,32 @@ __device__ __forceinline__ void items_kernel_body(const AttnArgs& a) {
   };
   // The queue: the current entry and the next one.  The one after is drawn while the current item is worked on (its first thread asks
   // for it at the start and leaves it in LDS before the item's last barrier).
-  const bool draws = total > 2 * grid;
+  // Apart, entries are the prefix items and then the suffix items, and the two kinds are drawn by themselves.
+  const bool draws = apart || total > 2 * grid;
   int cur = blockIdx.x, next = 2 * grid - 1 - cur, parity = 0, drawn = 0;
+  bool streams = false;   // (of the first thread: draws suffix items)
+  if (apart) {
+    streams = cur < streamers;
+    const int at = streams ? cur : cur - streamers, mirror = 2 * (streams ? streamers : others) - 1 - at;
+    cur = streams ? n_prefix + at : at < n_prefix ? at : total;
+    next = streams ? n_prefix + mirror : mirror < n_prefix ? mirror : total;
+  }
+  auto draw_prefix = [&] { return 2 * others + atomicAdd(&a.counters[MARL_CTR_PREFIX_CURSOR], 1); };
   auto draw = [&] {
-    if (draws && threadIdx.x == 0) drawn = 2 * grid + atomicAdd(&a.counters[MARL_CTR_SUFFIX_CURSOR], 1);
+    if (!draws || threadIdx.x != 0) return;
+    if (apart && !streams) drawn = draw_prefix();
+    else drawn = (apart ? n_prefix + 2 * streamers : 2 * grid) + atomicAdd(&a.counters[MARL_CTR_SUFFIX_CURSOR], 1);
   };
   auto leave_drawn = [&] {
-    if (draws && threadIdx.x == 0) drawn_entry[parity] = drawn;
+    if (!draws || threadIdx.x != 0) return;
+    if (apart) {
+      if (streams && drawn >= total) {   // no suffix item is left
+        streams = false;
+        drawn = draw_prefix();
+      }
+      if (!streams && drawn >= n_prefix) drawn = total;
+    }
+    drawn_entry[parity] = drawn;
   };
   auto advance = [&] {   // after the barrier
     cur = next;

@@ -168,6 +168,23 @@ def test_a_row_does_not_depend_on_its_place(members, alone, Hq, Hkv):
     assert np.array_equal(again, got[order.numpy()])
 
 
+@pytest.mark.parametrize("seqs,samples,prefix,chunk,Hq", [
+    (160, 160, [0], 32, 8),                                  # no prefix at all
+    (160, 4, list(range(1, 128, 3))[:40], 32, 8),            # up to four chunks a group
+    (200, 2, [128] * 100, 32, 4),                            # more prefix items than any two rounds of workgroups
+    (160, 80, [100, 33], 64, 8),                             # blocks of 256 query rows
+    (131, 131, [40], 64, 8)])
+def test_few_long_items_among_many(seqs, samples, prefix, chunk, Hq):
+    """Three suffix items that would end long after all others (4 KV heads, so 640 items and more): the kinds of items are drawn apart.
+    (131 sequences: 524 items.)"""
+    print("case: fp8 attention, few long items", seqs, len(prefix), flush=True)
+    rng = np.random.default_rng(seqs + len(prefix))
+    slens = rng.integers(129, 200, seqs)
+    slens[rng.permutation(seqs)[:3]] = [6000, 5003, 4100]
+    gos = rng.permutation(np.arange(seqs) // samples)
+    check(custom_inputs(prefix, slens, gos, Hq, 4, seed=seqs), suffix_chunk_tokens=8192, prefix_chunk_tokens=chunk)
+
+
 @pytest.mark.parametrize("name,pdiv,ldiv", [("tiny", 1, 1), ("qwen7b", 16, 4), ("skew", 8, 8), ("prefix", 16, 4), ("long32b", 8, 8)])
 def test_scaled_workloads(name, pdiv, ldiv):
     print("case: fp8 attention", name, flush=True)
