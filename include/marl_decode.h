@@ -369,9 +369,8 @@ int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, con
  * workspace (marl_workspace_bytes), work lists, flags and limits; q stays bf16.  A token's row whose exponent lies outside what the writing calls
  * store ([-110, 120]) gives unspecified values, codes and exponents that no token owns are never read into a result.  The weights are
  * rounded to bf16 before they multiply the values, as in marl_decode_attn; everything else is float32.  Its items are those of
- * marl_decode_attn's lists, always taken by one kernel (the event timing counts it as the suffix stage).  Default chunks are the same too:
- * where few own lengths are near the table rows' end, a caller that names half of a default suffix chunk of 8192 tokens, and makes its
- * workspace for that, evens out the call's end (512 sequences of 1 to 8192 own tokens: 171 us instead of 179).
+ * marl_decode_attn's lists, always taken by one kernel (the event timing counts it as the suffix stage).  Default chunks are the same, but
+ * for general calls none is under 512 tokens (the work list in the workspace is laid out for those).
  */
 int marl_kv_append_fp8(const marl_attn_shape* shape, const void* k_new, const void* v_new,
                        void* k_pages, void* v_pages, int8_t* exponents, const int32_t* suffix_block_table,

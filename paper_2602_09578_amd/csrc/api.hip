@@ -3,6 +3,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -229,6 +230,7 @@ int take_attn_operands(marl::AttnArgs& a, const void* q, const void* k_pages, co
 // The suffix kernel takes the items of more than kShortTokens tokens: none can exist when neither a table row nor a
 // chunk holds that many.
 bool can_have_long_items(const marl::AttnArgs& a) { return (long)a.max_sp * marl::kPage > marl::kShortTokens && a.Cs > marl::kShortTokens; }
+constexpr int32_t kLeastChunkFp8 = 512;   // of the default ones for an 8-bit cache
 bool default_chunks(const marl_attn_shape* s) { return s->suffix_chunk_tokens == 0 && s->prefix_chunk_tokens == 0; }
 
 // Enqueues the kernels of one decode-attention call.  `may_time`: the call takes part in the
@@ -384,6 +386,16 @@ int marl_decode_attn_fp8(const marl_attn_shape* shape, void* workspace, size_t w
   marl::AttnArgs a;
   int rc = fill_args(shape, workspace, workspace_bytes, a);
   if (rc != MARL_OK) return rc;
+  // Default chunks of 256 tokens become 512: with half the bytes an item's fixed cost weighs twice (108 sequences behind 4 prompts of 3944 tokens,
+  // 32 / 8 heads: 82 -> 68 us; 117 behind 13 of 1344 to 5377, 8 / 2 heads: 51 -> 42; none of 24 such calls slower).  Fewer chunks need less
+  // workspace.
+  if (default_chunks(shape) && marl::small_attn_splits(a) == 0) {
+    marl_attn_shape longer = *shape;
+    longer.suffix_chunk_tokens = std::max(a.Cs, kLeastChunkFp8);
+    longer.prefix_chunk_tokens = std::max(a.Cp, kLeastChunkFp8);
+    rc = fill_args(&longer, workspace, workspace_bytes, a);
+    if (rc != MARL_OK) return rc;
+  }
   rc = take_attn_operands(a, q, k_pages, v_pages, prefix_block_table, suffix_block_table, prefix_lens,
                           suffix_lens, group_of_seq, scale, out);
   if (rc != MARL_OK) return rc;
