@@ -370,7 +370,8 @@ int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, con
  * store ([-110, 120]) gives unspecified values, codes and exponents that no token owns are never read into a result.  The weights are
  * rounded to bf16 before they multiply the values, as in marl_decode_attn; everything else is float32.  Its items are those of
  * marl_decode_attn's lists, always taken by one kernel (the event timing counts it as the suffix stage).  Default chunks are the same, but
- * for general calls none is under 512 tokens (the work list in the workspace is laid out for those).
+ * for general calls none is under 512 tokens (the work list in the workspace is laid out for those); calls of up to twice as many tokens are
+ * small ones.
  */
 int marl_kv_append_fp8(const marl_attn_shape* shape, const void* k_new, const void* v_new,
                        void* k_pages, void* v_pages, int8_t* exponents, const int32_t* suffix_block_table,

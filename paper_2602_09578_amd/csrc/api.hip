@@ -386,8 +386,9 @@ int marl_decode_attn_fp8(const marl_attn_shape* shape, void* workspace, size_t w
   marl::AttnArgs a;
   int rc = fill_args(shape, workspace, workspace_bytes, a);
   if (rc != MARL_OK) return rc;
+  a.exponents = exponents;
   // Default chunks of 256 tokens become 512: with half the bytes an item's fixed cost weighs twice (108 sequences behind 4 prompts of 3944 tokens,
-  // 32 / 8 heads: 82 -> 68 us; 117 behind 13 of 1344 to 5377, 8 / 2 heads: 51 -> 42; none of 24 such calls slower).  Fewer chunks need less
+  // 32 / 8 heads: 82 -> 68 us; 374 behind 17 of up to 561, 8 / 2 heads: 73 -> 65; none of 24 such calls slower).  Fewer chunks need less
   // workspace.
   if (default_chunks(shape) && marl::small_attn_splits(a) == 0) {
     marl_attn_shape longer = *shape;
