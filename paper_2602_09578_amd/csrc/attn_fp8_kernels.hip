@@ -7,8 +7,7 @@
 // convert: so items follow each other without a gap, and waves without a row tile of their own share the others' tokens.
 //   Measured (a call; its plan, items and merge kernels): 128 sequences of 8192 to 24576 own tokens and 32 prefixes of 8192, 64 / 8 heads,
 // 4932 MB: 796 us (7, 781, 12; 6.3 TB/s in the items kernel, where the loads alone reach 6.8 and a plain read 7.0).  512 of a median of 256 to
-// 2048 (at most 8192) and 64 prefixes of 512 to 2048, 28 / 4 heads, 789 MB: 182 us (6, 162, 12): the longest item, one workgroup's share of the
-// memory's rate, ends last.
+// 2048 (at most 8192) and 64 prefixes of 512 to 2048, 28 / 4 heads, 789 MB: 169 us (6, 149, 12).
 #include <algorithm>
 #include <type_traits>
 
@@ -138,7 +137,7 @@ __device__ __forceinline__ SuffixItem suffix_item(const AttnArgs& a, int index) 
 //   Blocks of up to 256 rows (kHalves): half of the tiles each for two workgroups that run on the same XCD, as in attn_kernels.hip; their
 // keys and values are ordinary cached loads.
 //   What bounds them: the issue of instructions.  A step of a wave with two tiles is about 560 of them, 64 of these matrix instructions.  16 prefixes
-// of 4096 tokens for 224 rows, 4 KV heads, 30 GFLOP: 56 us in the items kernel (0.54 PFLOP/s), the same on pages that the caches hold.  Measured
+// of 4096 tokens for 224 rows, 4 KV heads, 30 GFLOP: 57 us in the items kernel (0.53 PFLOP/s), the same on pages that the caches hold.  Measured
 // and left out: scores by products of 8-bit numbers (the queries as two of them each: 71 us a call instead of 74, but calls bound by memory
 // 0.5 to 1 % slower), one half of a step's weights beside the other half's scores (3 % slower), chunks of twice the default (88 us).
 //   LDS: keys as 64 token rows of 128 bytes, the 16-byte chunk index XOR-ed with bits 1, 4, 5 of the row (the 16 rows of an operand read differ
