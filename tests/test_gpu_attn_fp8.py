@@ -1,8 +1,8 @@
-"""Decode attention over an 8-bit cache against the float64 checker on the values that the codes stand for, by every kernel route.
+"""Decode attention over an 8-bit cache against the float64 oracle on the values that the codes stand for, by every kernel route.
 
 Tolerance, element by element, from the operation: a weight is rounded to bf16 before it multiplies its value (to nearest of 8 significant bits: up to 2^-8 of it),
 and has the float32 error of its score, at most 128 * 2^-24 of the sum of |q k| scale (about 10 here, 80 with scale 1: 2^-13 and 2^-10 of the weight at
-most); so the error is at most (2^-8 + 2^-12) (scale 1: 2^-8 + 2^-10) of the weighted mean of the values' magnitudes, which the checker gives for the magnitudes as values.
+most); so the error is at most (2^-8 + 2^-12) (scale 1: 2^-8 + 2^-10) of the weighted mean of the values' magnitudes, which the oracle gives for the magnitudes as values.
 A bf16 output is rounded once more, 2^-8 of its value."""
 import numpy as np
 import pytest
