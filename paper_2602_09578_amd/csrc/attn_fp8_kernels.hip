@@ -6,8 +6,8 @@
 // With half the bytes per token the fixed costs of an item weigh twice as much as over a bf16 cache, and the vector ALU has codes to
 // convert: so items follow each other without a gap, and waves without a row tile of their own share the others' tokens.
 //   Measured (a call; its plan, items and merge kernels): 128 sequences of 8192 to 24576 own tokens and 32 prefixes of 8192, 64 / 8 heads,
-// 4932 MB: 796 us (7, 781, 12; 6.3 TB/s in the items kernel, where the loads alone reach 6.8 and a plain read 7.0).  512 of a median of 256 to
-// 2048 (at most 8192) and 64 prefixes of 512 to 2048, 28 / 4 heads, 789 MB: 169 us (6, 149, 12).
+// 4932 MB: 794 us (7, 780, 11; 6.3 TB/s in the items kernel, where the loads alone reach 6.8 and a plain read 7.0).  512 of a median of 256 to
+// 2048 (at most 8192) and 64 prefixes of 512 to 2048, 28 / 4 heads, 789 MB: 168 us (6, 149, 10).
 #include <algorithm>
 #include <type_traits>
 
@@ -24,6 +24,7 @@ constexpr int NW = kAttnThreads / 64;
 constexpr int kStride = NW * kStepTok;   // tokens that the waves of a workgroup take in turn
 constexpr int kMaximaAtOnce = 8;         // of partials that are about to be added
 constexpr int kEager = 4;                // partials of a row that are requested before the first is used
+constexpr int kSpareBlocks = 128;        // workgroups of the merge kernel beside those for the rows
 
 // The thread's index, as something that the compiler knows nothing of: what follows from it is formed where it is used, not once
 // for all items in registers that an item needs (which had 20 of them in scratch memory, and a launch with scratch takes 10 us longer).
@@ -756,82 +757,101 @@ void items_fp8_kernel(AttnArgs a) { items_kernel_body<false>(a); }
 __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void items_fp8_kernel_wide(AttnArgs a) { items_kernel_body<true>(a); }
 
-// Adds the partials of one row, those of npc prefix chunks and nsc own ones, in slot order, and stores the row; half a wave a row.
-__device__ __forceinline__ void merge_row(const AttnArgs& a, const int row, const int npc, const int nsc) {
-  const int sub = threadIdx.x & 31;   // lane within the half wave: channels 4*sub .. 4*sub+3
-  const int n = npc + nsc;
-  const int nslot = a.NCp + a.NCs;
-  const float2* ml = a.partial_ml + (size_t)row * nslot;
-  const float* po = a.partial_o + (size_t)row * nslot * kD + 4 * sub;
-  auto slot_of = [&](int k) { return k < npc ? k : a.NCp + (k - npc); };
-
+// The partials of one row, those of npc prefix chunks and nsc own ones, added in slot order; half a wave a row.
+struct MergedRow {
+  int row, npc, n;   // n < 0: not a row to be added
   float2 mlk[kEager];
   f32x4 ok[kEager];
-#pragma unroll
-  for (int k = 0; k < kEager; ++k) {
-    mlk[k] = make_float2(-INFINITY, 0.f);
-    ok[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (k < n) {
-      const int sl = slot_of(k);
-      mlk[k] = ml[sl];
-      ok[k] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(po + (size_t)sl * kD));
-    }
-  }
-  float mstar = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < kEager; ++k) mstar = fmaxf(mstar, mlk[k].x);
-  for (int k = kEager; k < n; k += kMaximaAtOnce) {
-    float mk[kMaximaAtOnce];
-#pragma unroll
-    for (int u = 0; u < kMaximaAtOnce; ++u) mk[u] = ml[slot_of(min(k + u, n - 1))].x;
-#pragma unroll
-    for (int u = 0; u < kMaximaAtOnce; ++u) mstar = fmaxf(mstar, mk[u]);
+
+  __device__ __forceinline__ int slot_of(const AttnArgs& a, int k) const { return k < npc ? k : a.NCp + (k - npc); }
+  __device__ __forceinline__ size_t first_slot(const AttnArgs& a) const { return (size_t)row * (a.NCp + a.NCs); }
+  // (channels 4*sub .. 4*sub+3 of the lane)
+  __device__ __forceinline__ f32x4 load(const AttnArgs& a, int slot) const {
+    return __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.partial_o + (first_slot(a) + slot) * kD + 4 * (threadIdx.x & 31)));
   }
 
-  float denom = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  // Asks for the first ones.
+  __device__ __forceinline__ void request(const AttnArgs& a, int r, bool here, int num_prefix, int num_own) {
+    row = r;
+    npc = num_prefix;
+    n = here ? num_prefix + num_own : -1;
 #pragma unroll
-  for (int k = 0; k < kEager; ++k) {
-    const float f = (mlk[k].x == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(mlk[k].x - mstar);
-    denom = __builtin_fmaf(mlk[k].y, f, denom);
-    acc += ok[k] * f;
-  }
-  for (int k = kEager; k < n; k += kEager) {   // as many at once as before the first use
-#pragma unroll
-    for (int u = 0; u < kEager; ++u) {
-      const int sl = slot_of(min(k + u, n - 1));
-      mlk[u] = ml[sl];
-      ok[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(po + (size_t)sl * kD));
-    }
-#pragma unroll
-    for (int u = 0; u < kEager; ++u) {
-      const float f = (mlk[u].x == -INFINITY || k + u >= n) ? 0.f : __builtin_amdgcn_exp2f(mlk[u].x - mstar);
-      denom = __builtin_fmaf(mlk[u].y, f, denom);
-      acc += ok[u] * f;
+    for (int k = 0; k < kEager; ++k) {
+      mlk[k] = make_float2(-INFINITY, 0.f);
+      ok[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (k < n) {
+        const int sl = slot_of(a, k);
+        mlk[k] = a.partial_ml[first_slot(a) + sl];
+        ok[k] = load(a, sl);
+      }
     }
   }
-  f32x4 r = {0.f, 0.f, 0.f, 0.f};
-  if (n > 0 && denom > 0.f) r = acc * (1.0f / denom);
-  store_row_piece(a, (size_t)row * kD + 4 * sub, r);
-}
+  // Adds all of them and stores the row.
+  __device__ __forceinline__ void finish(const AttnArgs& a) {
+    if (n < 0) return;
+    float mstar = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kEager; ++k) mstar = fmaxf(mstar, mlk[k].x);
+    for (int k = kEager; k < n; k += kMaximaAtOnce) {
+      float mk[kMaximaAtOnce];
+#pragma unroll
+      for (int u = 0; u < kMaximaAtOnce; ++u) mk[u] = a.partial_ml[first_slot(a) + slot_of(a, min(k + u, n - 1))].x;
+#pragma unroll
+      for (int u = 0; u < kMaximaAtOnce; ++u) mstar = fmaxf(mstar, mk[u]);
+    }
+    float denom = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kEager; ++k) {
+      const float f = (mlk[k].x == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(mlk[k].x - mstar);
+      denom = __builtin_fmaf(mlk[k].y, f, denom);
+      acc += ok[k] * f;
+    }
+    for (int k = kEager; k < n; k += kEager) {   // as many at once as before the first use
+#pragma unroll
+      for (int u = 0; u < kEager; ++u) {
+        const int sl = slot_of(a, min(k + u, n - 1));
+        mlk[u] = a.partial_ml[first_slot(a) + sl];
+        ok[u] = load(a, sl);
+      }
+#pragma unroll
+      for (int u = 0; u < kEager; ++u) {
+        const float f = (mlk[u].x == -INFINITY || k + u >= n) ? 0.f : __builtin_amdgcn_exp2f(mlk[u].x - mstar);
+        denom = __builtin_fmaf(mlk[u].y, f, denom);
+        acc += ok[u] * f;
+      }
+    }
+    f32x4 r = {0.f, 0.f, 0.f, 0.f};
+    if (n > 0 && denom > 0.f) r = acc * (1.0f / denom);
+    store_row_piece(a, (size_t)row * kD + 4 * (threadIdx.x & 31), r);
+  }
+};
 
 // Merge kernel: first the sequences whose own tokens are one short item, then the other rows' partials, half a wave a row.
-// What bounds it: chains of dependent loads (the lists' lengths, an item, its page ids, its keys, the prefix partials).  13 us for 8192 rows of up
-// to five partials, 13 for 14336 of up to three, 15 for 2048 items of up to 64 tokens with four prefix partials each.  Two to four rows for half a wave
+// What bounds it: chains of dependent loads (the lists' lengths, an item, its page ids, its keys, the prefix partials).  11 us for 8192 rows of up
+// to five partials, 10 for 14336 of up to three, 15 for 2048 items of up to 64 tokens with four prefix partials each.  Two to four rows for half a wave
 // at once were 1 to 3 us slower.
+// The workgroups that have short items take rows last, and the grid has some to spare, so that a row hardly ever waits for an item: 1 to 2 us
+// of a call.
 constexpr int kRowsPerBlock = kAttnThreads / 32;
 __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void merge_fp8_kernel(AttnArgs a) {
-  const int row = blockIdx.x * kRowsPerBlock + (threadIdx.x >> 5);
-  const int rows = a.NS * a.Hq, seq = min(row, rows - 1) / a.Hq;   // (loads without a branch, which would be waited for before the items)
+  const int rows = a.NS * a.Hq, at = blockIdx.x, grid = gridDim.x;
+  const int short_items = (a.counters[MARL_CTR_NUM_SUFFIX_ITEMS] - a.counters[MARL_CTR_NUM_LONG_SUFFIX_ITEMS]) * a.Hkv;
+  const int takers = min((short_items + NW - 1) / NW, grid);
+  const int row = (at >= takers ? at - takers : at + grid - takers) * kRowsPerBlock + (threadIdx.x >> 5);
+  const int seq = min(row, rows - 1) / a.Hq;   // (loads without a branch, which would be waited for before the items)
   const int info = a.seq_chunks[seq];
   const int own = min(a.suffix_lens[seq], a.max_sp * kPage);
   int bad_page = 0;
   short_suffix_items<true>(a, bad_page);
   if (bad_page) atomicOr(&a.counters[MARL_CTR_FLAGS], MARL_FLAG_BAD_PAGE);
   const int npc = info & 0xffff, nsc = info >> 16;
-  if (row >= rows || (nsc == 1 && (npc == 0 || own <= kShortTokens))) return;   // finished above, or in the items kernel
-  merge_row(a, row, npc, nsc);
+  // (else finished above, or in the items kernel)
+  const bool here = row < rows && !(nsc == 1 && (npc == 0 || own <= kShortTokens));
+  MergedRow m;
+  m.request(a, min(row, rows - 1), here, npc, nsc);
+  m.finish(a);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -922,8 +942,9 @@ hipError_t launch_items_fp8(const AttnArgs& a, int grid, hipStream_t st) {
 
 hipError_t launch_merge_fp8(const AttnArgs& a, hipStream_t st) {
   // (a wave for every short item)
-  const long rows = (long)a.NS * a.Hq;
-  const long grid = std::max((rows + kRowsPerBlock - 1) / kRowsPerBlock, ((long)a.NS * a.Hkv + NW - 1) / NW);
+  const long rows = (long)a.NS * a.Hq, waves = ((long)a.NS * a.Hkv + NW - 1) / NW;
+  const long row_blocks = (rows + kRowsPerBlock - 1) / kRowsPerBlock;
+  const long grid = std::max(row_blocks + std::min(waves, (long)kSpareBlocks), waves);
   hipLaunchKernelGGL(merge_fp8_kernel, dim3((unsigned)grid), dim3(kAttnThreads), 0, st, a);
   return hipGetLastError();
 }
