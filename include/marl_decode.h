@@ -372,6 +372,9 @@ int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, con
  * marl_decode_attn's lists, always taken by one kernel (the event timing counts it as the suffix stage).  Default chunks are the same, but
  * for general calls none is under 512 tokens (the work list in the workspace is laid out for those); calls of up to twice as many tokens are
  * small ones.
+ *
+ * A launch holds fewer than 2^24 workgroups: 2^24 sequences and more in an append, n * Hkv of 2^24 and more in a read, and in a
+ * general attention call more than 2^27 - 1032 rows (num_seqs * num_q_heads) or 2^26 - 4 (sequence, KV head) pairs are MARL_UNSUPPORTED.
  */
 int marl_kv_append_fp8(const marl_attn_shape* shape, const void* k_new, const void* v_new,
                        void* k_pages, void* v_pages, int8_t* exponents, const int32_t* suffix_block_table,
@@ -429,7 +432,8 @@ int marl_grpo_advantages(const float* rewards, const int32_t* group_start,
  *   dx_d = r (g_d - n_d sum_e g_e n_e / D)              -> dq, dk [.., dq_stride / dk_stride apart]; may be dq_out and dk_out
  *   dw_d = sum over tokens and heads of dy_d n_d        -> dq_weight, dk_weight float32 [D] (written, not added to; NULL: not wanted)
  * The sums are formed in float32 in an order that the shape alone decides: the same bits in every run.  num_tokens = 0 writes zeros to
- * dq_weight and dk_weight.  workspace: marl_qk_norm_rope_workspace_bytes() bytes, 16-byte aligned (needed by the backward call only).
+ * dq_weight and dk_weight.  A forward call takes groups of 512 / head_dim query heads, and of as many key heads, of a token, four of them a wave;
+ * more than 2^26 - 4 waves (so many tokens, where one wave takes a token) are MARL_UNSUPPORTED.  workspace: marl_qk_norm_rope_workspace_bytes() bytes, 16-byte aligned (needed by the backward call only).
  * Every array but positions is accessed in 16-byte vectors: pointers must be 16-byte aligned, and strides multiples of 16 bytes
  * (MARL_INVALID_ARG otherwise).
  */

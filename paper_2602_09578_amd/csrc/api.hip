@@ -402,6 +402,7 @@ int marl_decode_attn_fp8(const marl_attn_shape* shape, void* workspace, size_t w
   if (rc != MARL_OK) return rc;
   if (a.NS == 0) return MARL_OK;
   if (!exponents || !aligned16(exponents)) return MARL_INVALID_ARG;
+  if (!marl::merge_fp8_fits(a)) return MARL_UNSUPPORTED;
   a.exponents = exponents;
   return enqueue_decode_attn(a, default_chunks(shape), static_cast<hipStream_t>(stream), /*may_time=*/true);
 }
@@ -513,6 +514,7 @@ int marl_kv_append_fp8(const marl_attn_shape* shape, const void* k_new, const vo
   if (!k_new || !v_new || !k_pages || !v_pages || !exponents || !suffix_block_table || !suffix_lens) return MARL_INVALID_ARG;
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(exponents)) return MARL_INVALID_ARG;
   if (shape->max_suffix_pages < 1) return MARL_INVALID_ARG;
+  if (shape->num_seqs > marl::most_workgroups(marl::kAppendThreads)) return MARL_UNSUPPORTED;
   marl::KvAppendFp8Args a;
   a.k_new = static_cast<const uint16_t*>(k_new);
   a.v_new = static_cast<const uint16_t*>(v_new);
@@ -534,7 +536,7 @@ int marl_kv_read_pages_fp8(int32_t num_kv_heads, int32_t num_pages, const void* 
                            const int8_t* exponents, int32_t num_out_pages, void* k_pages, void* v_pages,
                            const int32_t* src, const int32_t* dst, int32_t n, int32_t* flags, void* stream) {
   if (num_kv_heads < 1 || num_pages < 1 || num_out_pages < 1 || n < 0) return MARL_INVALID_ARG;
-  if ((long)n * num_kv_heads >= (1L << 31)) return MARL_UNSUPPORTED;   // one workgroup per page and KV head
+  if ((long)n * num_kv_heads > marl::most_workgroups(marl::kReadPagesThreads)) return MARL_UNSUPPORTED;
   if (n == 0) return MARL_OK;
   if (!k_codes || !v_codes || !exponents || !k_pages || !v_pages || !src || !dst) return MARL_INVALID_ARG;
   if (!aligned16(k_codes) || !aligned16(v_codes) || !aligned16(exponents) || !aligned16(k_pages) || !aligned16(v_pages)) return MARL_INVALID_ARG;
@@ -945,6 +947,7 @@ int marl_qk_norm_rope(const marl_norm_rope_shape* shape, const void* q, const vo
   if (!norm_rope_rows_ok(shape, q_out, shape->q_out_stride, shape->num_q_heads, true) ||
       !norm_rope_rows_ok(shape, k_out, shape->k_out_stride, shape->num_kv_heads, true))
     return MARL_INVALID_ARG;
+  if (!marl::qk_norm_rope_fits(a)) return MARL_UNSUPPORTED;
   a.q_out = q_out;
   a.k_out = k_out;
   const hipError_t e = marl::launch_qk_norm_rope(a, static_cast<hipStream_t>(stream));

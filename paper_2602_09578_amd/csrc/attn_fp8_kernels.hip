@@ -940,12 +940,17 @@ hipError_t launch_items_fp8(const AttnArgs& a, int grid, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_merge_fp8(const AttnArgs& a, hipStream_t st) {
-  // (a wave for every short item)
+// (a wave for every short item)
+static long merge_workgroups(const AttnArgs& a) {
   const long rows = (long)a.NS * a.Hq, waves = ((long)a.NS * a.Hkv + NW - 1) / NW;
   const long row_blocks = (rows + kRowsPerBlock - 1) / kRowsPerBlock;
-  const long grid = std::max(row_blocks + std::min(waves, (long)kSpareBlocks), waves);
-  hipLaunchKernelGGL(merge_fp8_kernel, dim3((unsigned)grid), dim3(kAttnThreads), 0, st, a);
+  return std::max(row_blocks + std::min(waves, (long)kSpareBlocks), waves);
+}
+
+bool merge_fp8_fits(const AttnArgs& a) { return merge_workgroups(a) <= most_workgroups(kAttnThreads); }
+
+hipError_t launch_merge_fp8(const AttnArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(merge_fp8_kernel, dim3((unsigned)merge_workgroups(a)), dim3(kAttnThreads), 0, st, a);
   return hipGetLastError();
 }
 

@@ -18,7 +18,6 @@ namespace {
 // the first store (64 sequences, 8 KV heads: 5.2 us; one head after the other, each waiting for its
 // loads, 7.8 us).  Every thread reads the old length before the barrier; thread 0 stores the new
 // one after it.
-constexpr int kAppendThreads = 256;
 __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(KvAppendArgs a) {
   const int s = blockIdx.x;
   const int tid = threadIdx.x;
@@ -102,7 +101,7 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_fp8_kernel(KvAppendF
 // whoever reads it next.
 constexpr long kReadCacheBytes = 32l << 20;
 template <bool kPastCaches>
-__global__ __launch_bounds__(256) void kv_read_pages_fp8_kernel(KvReadFp8Args a) {
+__global__ __launch_bounds__(kReadPagesThreads) void kv_read_pages_fp8_kernel(KvReadFp8Args a) {
   const int pair = blockIdx.x / a.Hkv, h = blockIdx.x - pair * a.Hkv, t = threadIdx.x;
   const int src = a.src[pair], dst = a.dst[pair];
   if ((unsigned)src >= (unsigned)a.num_pages || (unsigned)dst >= (unsigned)a.num_out_pages) {
@@ -168,7 +167,7 @@ hipError_t launch_kv_append_fp8(const KvAppendFp8Args& a, hipStream_t st) {
 hipError_t launch_kv_read_pages_fp8(const KvReadFp8Args& a, hipStream_t st) {
   if (a.n == 0) return hipSuccess;
   const bool past_caches = (long)a.n * a.Hkv * (2 * kPage * kD * 2) > kReadCacheBytes;
-  hipLaunchKernelGGL(past_caches ? kv_read_pages_fp8_kernel<true> : kv_read_pages_fp8_kernel<false>, dim3((unsigned)(a.n * a.Hkv)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(past_caches ? kv_read_pages_fp8_kernel<true> : kv_read_pages_fp8_kernel<false>, dim3((unsigned)(a.n * a.Hkv)), dim3(kReadPagesThreads), 0, st, a);
   return hipGetLastError();
 }
 

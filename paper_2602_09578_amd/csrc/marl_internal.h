@@ -23,6 +23,8 @@ constexpr int kPrefixTokenCost = 4;   // time of a prefix item's token in tokens
 constexpr int kOneQueueItems = 6144;  // most (sequence, KV head) pairs of a call whose prefix and suffix items share a launch
 constexpr int kPlanThreads = 1024;
 constexpr int kNumClasses = 2048;  // upper bound on cost classes (chunk / 32)
+// Workgroups that one launch can have: a dispatch holds fewer than 2^32 threads.
+constexpr long most_workgroups(int threads) { return ((1l << 32) - 1) / threads; }
 
 // Everything the attention kernels need; passed by value.
 struct AttnArgs {
@@ -74,6 +76,7 @@ hipError_t launch_items_fp8(const AttnArgs& a, int grid, hipStream_t st);
 hipError_t launch_merge_fp8(const AttnArgs& a, hipStream_t st);
 hipError_t launch_small_attn_fp8(const AttnArgs& a, hipStream_t st);
 int items_fp8_blocks_per_cu(bool wide);
+bool merge_fp8_fits(const AttnArgs& a);   // one launch
 
 struct KvAppendArgs {
   const uint16_t* k_new;
@@ -116,6 +119,7 @@ struct KvReadFp8Args {
   int32_t* flags;      // may be null
   int32_t n, Hkv, num_pages, num_out_pages;
 };
+constexpr int kAppendThreads = 256, kReadPagesThreads = 256;   // one workgroup per sequence; per (page, KV head)
 hipError_t launch_kv_append_fp8(const KvAppendFp8Args& a, hipStream_t st);
 hipError_t launch_kv_read_pages_fp8(const KvReadFp8Args& a, hipStream_t st);
 hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st);
@@ -236,6 +240,7 @@ struct NormRopeArgs {
   bool f32, adjacent;
 };
 constexpr int kNormRopeMaxBlocks = 1024;   // workgroups of a backward call, each of which leaves a partial sum of dw
+bool qk_norm_rope_fits(const NormRopeArgs& a);   // the forward call in one launch (the backward kernel's workgroups stay)
 hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t st);
 hipError_t launch_qk_norm_rope_backward(const NormRopeArgs& a, hipStream_t st);
 

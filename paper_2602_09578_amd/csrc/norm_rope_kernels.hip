@@ -331,10 +331,13 @@ bool past_caches(const NormRopeArgs& a) { return (long)a.T * (a.Hq + a.Hkv) * a.
 
 int steps_of(const NormRopeArgs& a) { const int heads = 512 / a.D; return (a.Hq + heads - 1) / heads + (a.Hkv + heads - 1) / heads; }
 
+// Units of a forward call where a wave has `steps` steps at once.
+long units_of(const NormRopeArgs& a, int steps) { return (long)a.T * ((steps_of(a) + steps - 1) / steps); }
+
 template <bool kF32, int D, bool kAdjacent>
 hipError_t launch_forward(NormRopeArgs a, hipStream_t st) {
   const long all = steps_of(a);
-  const bool many = (long)a.T * ((all + kManySteps - 1) / kManySteps) >= kEnoughUnits;
+  const bool many = units_of(a, kManySteps) >= kEnoughUnits;
   const int steps = many ? kManySteps : kFewSteps;
   a.units_per_token = (int)((all + steps - 1) / steps);
   a.units = (int)((long)a.T * a.units_per_token);
@@ -377,6 +380,8 @@ hipError_t by_type(const NormRopeArgs& a, F&& launch) {
 }
 
 }  // namespace
+
+bool qk_norm_rope_fits(const NormRopeArgs& a) { return units_of(a, kManySteps) <= most_workgroups(kThreads) * kWavesPerBlock; }
 
 hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t st) {
   return by_type(a, [&](auto f32, auto dim, auto adjacent) {
