@@ -338,7 +338,7 @@ int marl_prefill_attn(const marl_prefill_shape* shape, void* workspace, size_t w
  * (MARL_FLAG_LEN_CLAMPED), a group with an inconsistent q_start / q_pos0 entry
  * (MARL_FLAG_BAD_GROUP), a page id out of range (MARL_FLAG_BAD_PAGE).  Bit-exact data movement.
  * k_new, k_pages and v_pages must be 16-byte aligned (MARL_INVALID_ARG otherwise): keys are
- * copied, and whole value pages stored, as 16-byte vectors.
+ * copied, and whole value pages stored, as 16-byte vectors.  More than 2^25 - 1 (group, KV head) pairs are MARL_UNSUPPORTED.
  */
 int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, const void* v_new,
                          void* k_pages, void* v_pages, const int32_t* prefix_block_table,

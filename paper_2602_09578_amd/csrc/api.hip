@@ -843,6 +843,7 @@ static int write_prompt(const marl_prefill_shape* shape, const void* k_new, cons
   a.q_start = q_start;
   a.q_pos0 = q_pos0;
   a.flags = flags;
+  if (!marl::kv_write_prompt_fits(a)) return MARL_UNSUPPORTED;
   const hipError_t e = marl::launch_kv_write_prompt(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? MARL_OK : hip_fail(e, "prompt scatter kernel");
 }

@@ -204,6 +204,7 @@ PrefillSplitLayout prefill_split_layout(long max_blocks, long Hkv, long max_keys
 int prefill_rows_per_block();
 int prefill_blocks_per_cu();
 hipError_t launch_prefill(const PrefillArgs& a, int grid, hipStream_t st);
+bool kv_write_prompt_fits(const PrefillArgs& a);   // one launch
 hipError_t launch_kv_write_prompt(const PrefillArgs& a, hipStream_t st);
 
 struct GrpoArgs {

@@ -1197,8 +1197,9 @@ hipError_t launch_prefill(const PrefillArgs& a, int grid, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_kv_write_prompt(const PrefillArgs& a, hipStream_t st) {
-  if (a.NT == 0 || a.NG == 0) return hipSuccess;
+// How a prompt scatter is launched: by places (cols = 0), or with `cols` workgroups per (group, KV head).
+struct PromptGrid { long cols, workgroups; };
+static PromptGrid prompt_grid(const PrefillArgs& a) {
   // How long a chunk is the host does not know, only what there is together and how wide the tables are.
   //   1. Every column that a chunk may touch has a workgroup where that leaves few without work (0.3 us a thousand), or where
   // memory hides them: 256 chunks of up to 1500, 64 / 8 heads, 364 us, by places 400; 900 of up to 600 behind up to 300 556 and 931.
@@ -1214,13 +1215,26 @@ hipError_t launch_kv_write_prompt(const PrefillArgs& a, hipStream_t st) {
   const bool few_empty = a.NG * all * a.Hkv <= 2048 || a.NG * all <= (places * a.Hkv >= 8192 ? 4 : 2) * places;
   long cols = few_empty ? all : std::min(all, 2 * mean + 2);
   const bool short_rounds = (all + cols - 1) / cols * (8 * 1100) <= places * a.Hkv * 3;   // ns; 16 KB at 5 TB/s a place and head
-  const bool fp8 = a.exponents_w != nullptr;
-  if (few_empty || short_rounds || a.NG > kScatterGroups)
-    hipLaunchKernelGGL(fp8 ? (cols == a.max_pp ? kv_write_prompt_kernel<true, true> : kv_write_prompt_kernel<false, true>)
-                           : (cols == a.max_pp ? kv_write_prompt_kernel<true, false> : kv_write_prompt_kernel<false, false>),
-                       dim3((unsigned)(a.NG * a.Hkv * cols)), dim3(kD), 0, st, a, (int)cols);
+  // (what one launch cannot hold goes round too: half a million groups of 8 columns, 8 KV heads)
+  constexpr long kMost = most_workgroups(kD);
+  const long pairs = (long)a.NG * a.Hkv;
+  if (!few_empty && !short_rounds && a.NG <= kScatterGroups && places * a.Hkv <= kMost) return {0, places * a.Hkv};
+  cols = std::max(std::min(cols, kMost / pairs), 1l);
+  return {cols, pairs * cols};
+}
+
+bool kv_write_prompt_fits(const PrefillArgs& a) { return prompt_grid(a).workgroups <= most_workgroups(kD); }
+
+hipError_t launch_kv_write_prompt(const PrefillArgs& a, hipStream_t st) {
+  if (a.NT == 0 || a.NG == 0) return hipSuccess;
+  const PromptGrid g = prompt_grid(a);
+  const bool fp8 = a.exponents_w != nullptr, every = g.cols == a.max_pp;
+  if (g.cols > 0)
+    hipLaunchKernelGGL(fp8 ? (every ? kv_write_prompt_kernel<true, true> : kv_write_prompt_kernel<false, true>)
+                           : (every ? kv_write_prompt_kernel<true, false> : kv_write_prompt_kernel<false, false>),
+                       dim3((unsigned)g.workgroups), dim3(kD), 0, st, a, (int)g.cols);
   else
-    hipLaunchKernelGGL(fp8 ? kv_write_prompt_pages_kernel<true> : kv_write_prompt_pages_kernel<false>, dim3((unsigned)(places * a.Hkv)), dim3(kD), a.NG <= 64 ? 0 : sizeof(int4) * a.NG, st, a);
+    hipLaunchKernelGGL(fp8 ? kv_write_prompt_pages_kernel<true> : kv_write_prompt_pages_kernel<false>, dim3((unsigned)g.workgroups), dim3(kD), a.NG <= 64 ? 0 : sizeof(int4) * a.NG, st, a);
   return hipGetLastError();
 }
 

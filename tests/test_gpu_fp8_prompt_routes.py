@@ -94,3 +94,13 @@ def test_pages_that_are_none(groups):
     print("case: fp8 prompt, bad pages", groups, flush=True)
     check(8, [900] + [33] * (groups - 1), [0] + [2000] * (groups - 1), "places",
           bad_pages=[(0, 3), (0, 4), (0, 56), (5, 125), (9, 127), (groups - 1, 126)], flag=B.FLAG_BAD_PAGE)
+
+
+def test_more_columns_than_a_launch_has_workgroups():
+    """Half a million groups of eight columns, eight KV heads: one column too many for a launch, so a chunk of eight goes round."""
+    print("case: fp8 prompt, 2^19 groups", flush=True)
+    NG = 1 << 19
+    chunks, ctx = np.zeros(NG, int), np.zeros(NG, int)
+    chunks[[7, 8, 300000, NG - 1]], ctx[[7, 300000, NG - 1]] = [120, 1, 40, 128], [3, 80, 0]
+    assert way(int(chunks.sum()), NG, 8, 8)[1] == 7
+    check(8, chunks, ctx, "rounds")

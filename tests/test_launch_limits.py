@@ -39,3 +39,12 @@ def test_norm(p, T, Hq, Hkv, D):
     per_token = -(-(-(-Hq * D // 512) + -(-Hkv * D // 512)) // 4)
     assert T * per_token > 4 * (LAUNCH - 1)
     assert B.load_library().marl_qk_norm_rope(ctypes.byref(s), *[p] * 8, None, None) == UNSUPPORTED
+
+
+# (128 threads a workgroup)
+@pytest.mark.parametrize("NG,Hkv", [(LAUNCH, 2), (2 * LAUNCH, 1)])
+def test_prompt(p, NG, Hkv):
+    s = B.make_prefill_shape(5, NG, Hkv, Hkv, 3, 1)
+    lib = B.load_library()
+    assert lib.marl_kv_write_prompt_fp8(ctypes.byref(s), *[p] * 8, None, None) == UNSUPPORTED
+    assert lib.marl_kv_write_prompt(ctypes.byref(s), *[p] * 7, None, None) == UNSUPPORTED
