@@ -371,7 +371,7 @@ int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, con
  * rounded to bf16 before they multiply the values, as in marl_decode_attn; everything else is float32.  Its items are those of
  * marl_decode_attn's lists, always taken by one kernel (the event timing counts it as the suffix stage).  Default chunks are the same, but
  * for general calls none is under 512 tokens (the work list in the workspace is laid out for those); calls of up to twice as many tokens are
- * small ones.
+ * small ones, where a sequence's table rows hold less than 2^20 of them.
  *
  * A launch holds fewer than 2^24 workgroups: 2^24 sequences and more in an append, n * Hkv of 2^24 and more in a read, and in a
  * general attention call more than 2^27 - 1032 rows (num_seqs * num_q_heads) or 2^26 - 4 (sequence, KV head) pairs are MARL_UNSUPPORTED.

@@ -265,6 +265,10 @@ int small_attn_splits(const AttnArgs& a) {
   // an 8-bit cache has half the bytes a token, so twice the tokens are a small call (of 16 drawn calls between the limits 12 are 1.05 to 1.6
   // times as fast and four 1 to 7 % slower; between twice and four times as many most are slower)
   const long bytes = a.exponents ? 2 : 1;
+  // ... but not in rows of a million tokens, 65536 a part, of which the limits leave one or two: two (sequence, KV head) pairs of 1 M own tokens 390 -> 324 us
+  // by the general kernels, one of 2 M 775 -> 518, as a prefix 775 -> 258, of 1 M as a prefix 350 -> 239 (own tokens 350 -> 435; 100 tokens in such
+  // a row 8.5 -> 11); rows of 768 K are 1.23 to 1.45 times as fast here but for a prefix of two heads (0.79) and three pairs (0.88)
+  if (a.exponents && prefix + own >= 1l << 20) return 0;
   if (items * (prefix + own) > (3l << 19) * bytes || items * prefix > (1l << 20) * bytes) return 0;
   if (prefix + own < 1024) return 1;
   const long n = std::min({(prefix + own) / 384, 1536 / items, 16l, (long)a.NCp + a.NCs});
