@@ -16,6 +16,7 @@ import sys
 from types import SimpleNamespace
 
 import torch
+from torch.autograd.function import once_differentiable
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2602_09578_amd import binding as B  # noqa: E402
@@ -46,7 +47,7 @@ class Layer:
 
 
 class QkNormRope(torch.autograd.Function):
-    """marl_qk_norm_rope with its gradient."""
+    """marl_qk_norm_rope with its gradient.  A weight may be None (ones); there is no second derivative."""
 
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, cos_sin, positions):
@@ -55,13 +56,16 @@ class QkNormRope(torch.autograd.Function):
         return B.marl_qk_norm_rope(q, k, q_weight, k_weight, cos_sin, positions, EPS, q_out, k_out)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq_out, dk_out):
         q, k, q_weight, k_weight, cos_sin, positions = ctx.saved_tensors
+        wanted = ctx.needs_input_grad
         dq, dk = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
-        dqw, dkw = (torch.empty(D, dtype=torch.float32, device=q.device) for _ in range(2))
+        dqw, dkw = (torch.empty(D, dtype=torch.float32, device=q.device) if w else None for w in wanted[2:4])   # (a call writes dq and dk always)
         ws = B.alloc_workspace(B.marl_qk_norm_rope_workspace_bytes(q.shape[0], q.shape[1], k.shape[1], D), q.device)
         B.marl_qk_norm_rope_backward(dq_out.contiguous(), dk_out.contiguous(), q, k, q_weight, k_weight, cos_sin, positions, EPS, dq, dk, dqw, dkw, ws)
-        return dq, dk, dqw.to(q_weight.dtype), dkw.to(k_weight.dtype), None, None
+        return (dq if wanted[0] else None, dk if wanted[1] else None, dqw.to(q_weight.dtype) if wanted[2] else None,
+                dkw.to(k_weight.dtype) if wanted[3] else None, None, None)
 
 
 def write_prompts(layer, cache, table, lens, x):
