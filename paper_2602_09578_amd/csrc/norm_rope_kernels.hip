@@ -62,7 +62,7 @@ struct Piece<true> {
     }
     return o;
   }
-  template <bool>
+  template <bool kPastCaches>   // (a lane's two stores are half of a line each, which the caches put together)
   static __device__ __forceinline__ void store(char* p, const float (&v)[8]) {
     *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
     *reinterpret_cast<f32x4*>(p + 16) = f32x4{v[4], v[5], v[6], v[7]};
@@ -324,10 +324,10 @@ __global__ __launch_bounds__(kFinishThreads) void qk_norm_weight_grad_kernel(Nor
 // + 4 heads of 128, two 169 instead of 161 for the gradient of 32771); few, where a call is small and waits for its loads.
 constexpr int kManySteps = 4, kFewSteps = 2, kBackwardSteps = 4, kBackwardStepsF32 = 2;
 constexpr long kEnoughUnits = 8192;
-// Results that the caches of the XCDs (4 MB each) cannot hold until somebody reads them are stored past them: 194 -> 187 us for the
+// bf16 results that the caches of the XCDs (4 MB each) cannot hold until somebody reads them are stored past them: 194 -> 187 us for the
 // 65543 tokens, 170 -> 161 for the gradient of 32771.
 constexpr long kCacheBytes = 32l << 20;
-bool past_caches(const NormRopeArgs& a) { return (long)a.T * (a.Hq + a.Hkv) * a.D * (a.f32 ? 4 : 2) > kCacheBytes; }
+bool past_caches(const NormRopeArgs& a) { return !a.f32 && (long)a.T * (a.Hq + a.Hkv) * a.D * 2 > kCacheBytes; }
 
 int steps_of(const NormRopeArgs& a) { const int heads = 512 / a.D; return (a.Hq + heads - 1) / heads + (a.Hkv + heads - 1) / heads; }
 
@@ -342,8 +342,8 @@ hipError_t launch_forward(NormRopeArgs a, hipStream_t st) {
   a.units_per_token = (int)((all + steps - 1) / steps);
   a.units = (int)((long)a.T * a.units_per_token);
   const dim3 grid((unsigned)((a.units + kWavesPerBlock - 1) / kWavesPerBlock));
-  // (few steps, 8192 units of them or fewer: at most 16 MB)
-  if (many && past_caches(a)) hipLaunchKernelGGL((qk_norm_rope_kernel<kF32, D, kAdjacent, kManySteps, true>), grid, dim3(kThreads), 0, st, a);
+  // (few steps: under 8192 units of four, so at most 32 MB in bf16)
+  if (many && past_caches(a)) hipLaunchKernelGGL((qk_norm_rope_kernel<kF32, D, kAdjacent, kManySteps, !kF32>), grid, dim3(kThreads), 0, st, a);
   else if (many) hipLaunchKernelGGL((qk_norm_rope_kernel<kF32, D, kAdjacent, kManySteps, false>), grid, dim3(kThreads), 0, st, a);
   else hipLaunchKernelGGL((qk_norm_rope_kernel<kF32, D, kAdjacent, kFewSteps, false>), grid, dim3(kThreads), 0, st, a);
   return hipGetLastError();
@@ -356,7 +356,7 @@ hipError_t launch_backward(NormRopeArgs a, hipStream_t st) {
   a.units = (int)((long)a.T * a.units_per_token);
   const int blocks = std::min((a.units + kWavesPerBlock - 1) / kWavesPerBlock, kNormRopeMaxBlocks);
   if (blocks > 0) {
-    if (past_caches(a)) hipLaunchKernelGGL((qk_norm_rope_backward_kernel<kF32, D, kAdjacent, kSteps, true>), dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
+    if (past_caches(a)) hipLaunchKernelGGL((qk_norm_rope_backward_kernel<kF32, D, kAdjacent, kSteps, !kF32>), dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
     else hipLaunchKernelGGL((qk_norm_rope_backward_kernel<kF32, D, kAdjacent, kSteps, false>), dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
