@@ -32,3 +32,46 @@ def test_rows_of_a_million_tokens(seqs, Hkv, prefix_pages, suffix_pages, stages)
     print("case: fp8 attention, wide rows", seqs, prefix_pages, suffix_pages, flush=True)
     c, _ = check(widen(custom_inputs([50], [4000, 33][:seqs], [0] * seqs, 4, Hkv, seed=5), prefix_pages, suffix_pages))
     assert c.stages() == stages
+
+
+DEFAULTS = [  # prompts' lengths, samples, Hq, Hkv, pages of the tables, the shape's default chunks, rows of a prefix block
+    ("wide blocks, own chunks of 256", [1500, 909], 20, 28, 4, 1024, 128, (256, 512), 256),
+    ("wide blocks, prefix chunks of 256", [2001, 600], 40, 16, 4, 420, 200, (512, 256), 256),
+    ("narrow blocks, both of 256", [1400, 0, 700, 4100], 16, 8, 8, 257, 32, (256, 256), 128),
+    ("narrow blocks, one prompt", [900], 70, 6, 6, 600, 20, (256, 256), 128),
+]
+
+
+@pytest.mark.parametrize("case", DEFAULTS, ids=[c[0] for c in DEFAULTS])
+def test_default_chunks_of_256_become_512(case):
+    """General calls with default chunks, in a workspace of the size that the shape has: the results, and the bits of a call that names chunks of 512."""
+    name, prompts, samples, Hq, Hkv, prefix_pages, suffix_pages, chunks, block = case
+    print("case: fp8 attention, default chunks,", name, flush=True)
+    rng = np.random.default_rng(samples)
+    gos = rng.permutation(np.repeat(np.arange(len(prompts)), samples))
+    slens = rng.choice([0, 1, 64, 127, 128, 129, 200, 256, 257, 320], size=len(gos))
+    slens[:4] = [320, 300, 0, 257]
+    inp = widen(custom_inputs(prompts, slens, gos, Hq, Hkv, seed=samples), prefix_pages, suffix_pages)
+    c, got = check(inp)
+    assert c.stages() == GENERAL
+    call = B.prepare_attn(c.dev, B.MARL_OUT_F32)
+    L = B.marl_attn_plan_layout_for(call.shape)
+    assert (L.suffix_chunk_tokens, L.prefix_chunk_tokens, L.rows_per_qblock) == (*chunks, block)
+    assert call.workspace.numel() == B.marl_workspace_bytes(call.shape) == L.total_bytes
+    named, _ = c.run(suffix_chunk_tokens=512, prefix_chunk_tokens=max(512, chunks[1]))
+    assert np.array_equal(got, named)
+    # the bf16 call on the same values: weights are rounded alike, only the sums' order differs
+    dev = c.bf16.to("cuda")
+    other = B.prepare_attn(dev, B.MARL_OUT_F32)
+    B.run_attn(dev, other)
+    torch.cuda.synchronize()
+    assert (np.abs(got - other.out.cpu().numpy()) <= 2 * (2.0 ** -8 + 2.0 ** -12) * c.magnitude()).all()
+
+
+@pytest.mark.parametrize("prompt,samples,Hq,Hkv", [(20001, 3, 4, 1), (40000, 3, 14, 2), (16200, 20, 4, 1), (36999, 40, 4, 2), (20500, 100, 4, 2)])
+def test_prefix_items_of_more_than_256_steps(prompt, samples, Hq, Hkv):
+    """Named prefix chunks of 65536 tokens: the list of an item's blocks, which holds 256 steps, is filled again while it runs; one to eight row tiles, and blocks of 256 rows."""
+    print("case: fp8 attention, long prefix items", prompt, samples, flush=True)
+    rng = np.random.default_rng(samples)
+    inp = custom_inputs([prompt, 16140], rng.integers(0, 140, samples + 2), [0] * samples + [1, 1], Hq, Hkv, seed=prompt)
+    check(inp, suffix_chunk_tokens=512, prefix_chunk_tokens=65536)
