@@ -368,7 +368,9 @@ int marl_kv_write_prompt(const marl_prefill_shape* shape, const void* k_new, con
  * marl_decode_attn_fp8: marl_decode_attn over such a cache: the same operation on the values that the codes stand for, the same shape,
  * workspace (marl_workspace_bytes), work lists, flags and limits; q stays bf16.  A token's row whose exponent lies outside what the writing calls
  * store ([-110, 120]) gives unspecified values, codes and exponents that no token owns are never read into a result.  The weights are
- * rounded to bf16 before they multiply the values, as in marl_decode_attn; everything else is float32.  Its items are those of
+ * rounded to bf16 before they multiply the values, as in marl_decode_attn; everything else is float32.  The weighted values are summed before they are
+ * divided by the weights' sum, with weights of at most 1 of a sequence's own tokens and of at most 64 on the mean of a prefix's: results are finite for values of
+ * magnitudes below 2^100 and up to 2^21 tokens, beyond that the sums may overflow.  Its items are those of
  * marl_decode_attn's lists, always taken by one kernel (the event timing counts it as the suffix stage).  Default chunks are the same, but
  * for general calls none is under 512 tokens (the work list in the workspace is laid out for those); calls of up to twice as many tokens are
  * small ones, where a sequence's table rows hold less than 2^20 of them.

@@ -134,7 +134,8 @@ __device__ __forceinline__ SuffixItem suffix_item(const AttnArgs& a, int index) 
 // are then added through the ring's LDS.  (All waves with the same tokens: 145 us instead of 110 for a call over 32 prefixes of 8192 tokens
 // for 32 rows each, 8 KV heads.)
 //   A row's reference maximum moves only when a lane's weights of that row in a step sum to more than kMaxWeight (none exceeds a sum that passes, and their
-// rounding to bf16 is relative): in the first step and hardly ever after.
+// rounding to bf16 is relative): in the first step and hardly ever after.  A lane takes four tokens at a time or more, so weights are at most 64 on the mean, and
+// sums over 2^21 tokens finite for values below 2^100.
 //   Blocks of up to 256 rows (kHalves): half of the tiles each for two workgroups that run on the same XCD, as in attn_kernels.hip; their
 // keys and values are ordinary cached loads.
 //   What bounds them: the issue of instructions.  A step of a wave with two tiles is about 560 of them, 64 of these matrix instructions.  16 prefixes

@@ -51,7 +51,8 @@ __device__ __forceinline__ uint32_t value_mask(int left, int d) {
   return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : 0xffffffffu >> (32 - 8 * n);
 }
 
-// Two words of the second product's operand: four weights times their values' scales.
+// Two words of the second product's operand: four weights times their values' scales.  The product takes bf16: a weight loses up to 2^-8 of itself, as
+// over a bf16 cache (its sum, the divisor, does not); held in two bf16 numbers each, weights would need twice the matrix instructions and registers.
 __device__ __forceinline__ void scaled_weights(const float* p, uint32_t exponents, uint32_t& lo, uint32_t& hi) {
   float w[4];
 #pragma unroll

@@ -7,6 +7,7 @@ import torch
 
 from paper_2602_09578_amd import binding as B
 from paper_2602_09578_amd import inputs as I
+from tests import fp8_cache_ref as fp8
 from tests.test_gpu_attn import custom_inputs
 from tests.test_gpu_attn_fp8 import PARTS, Cache, check
 
@@ -75,3 +76,29 @@ def test_prefix_items_of_more_than_256_steps(prompt, samples, Hq, Hkv):
     rng = np.random.default_rng(samples)
     inp = custom_inputs([prompt, 16140], rng.integers(0, 140, samples + 2), [0] * samples + [1, 1], Hq, Hkv, seed=prompt)
     check(inp, suffix_chunk_tokens=512, prefix_chunk_tokens=65536)
+
+
+@pytest.mark.parametrize("prefix_chunk", [96, 8192])
+def test_large_values_under_large_weights(prefix_chunk):
+    """Values just below 2^100, where results are finite by the header: a prefix whose scores rise by 4.9 after its first tokens, so that weights reach 30 and lanes' sums
+    240 of the 256 that they may have before the reference maximum moves."""
+    print("case: fp8 attention, large values", prefix_chunk, flush=True)
+    inp = custom_inputs([6000, 700], [0, 50, 3, 129], [0, 0, 1, 1], 14, 2, seed=8, poison=False)
+    inp.q[:] = 0.0
+    inp.q[:, :, 0] = 1.0
+    inp.scale = 4.9 / 1.4426950408889634
+    for g, n in ((0, 6000), (1, 700)):
+        pages = inp.prefix_block_table[g, : -(-n // 16)].long()
+        inp.k_pages[pages] = 1.0
+        inp.k_pages[pages[:6]] = 0.0
+    c = Cache(inp, spread=False)
+    c.ex[:, :, 1, :] = 91
+    v = c.v.view(torch.uint8)
+    v |= 0x70                                              # codes of 128 to 448
+    v &= 0x7f
+    v[v == 0x7f] = 0x7e
+    c.bf16.v_pages = torch.from_numpy(fp8.values(v.cpu().numpy(), c.ex.cpu().numpy()).astype(np.float32)).to(torch.bfloat16)
+    for chunks in ({}, dict(suffix_chunk_tokens=64, prefix_chunk_tokens=prefix_chunk)):
+        got, _ = c.run(**chunks)
+        assert np.isfinite(got).all() and np.abs(got).max() > 2.0 ** 97
+        assert (np.abs(got - c.want()) <= (2.0 ** -8 + 2.0 ** -12) * c.magnitude()).all()
