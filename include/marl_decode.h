@@ -413,7 +413,8 @@ int marl_grpo_advantages(const float* rewards, const int32_t* group_start,
 
 /*
  * Norm of every query and key head and rotation by position, in one pass over the heads: what stands between the projections
- * and the attention (or the cache) in the models that the paper trains.  For a head's row x of D = head_dim channels with its
+ * and the attention (or the cache) in models that normalise their query and key heads.  (Models that only rotate them, as those that the
+ * paper trains, have no use for this call: it always divides by the root mean square.)  For a head's row x of D = head_dim channels with its
  * weight w (q_weight for query heads, k_weight for key heads):
  *   r = 1 / sqrt(sum_d x_d^2 / D + eps),   y_d = x_d r w_d,
  * and with rotary_dim = 2 h, cos and sin of the token's position t: c_i = cos_sin[t][i], s_i = cos_sin[t][h + i], for i < h
@@ -427,7 +428,8 @@ int marl_grpo_advantages(const float* rewards, const int32_t* group_start,
  *   q_out, k_out     the results, q_out_stride / k_out_stride apart; may be q and k themselves (with their strides)
  * A position outside [0, max_positions) takes the nearest row of the table and sets MARL_FLAG_BAD_POSITION in *flags (device
  * int32, may be NULL; OR-ed, the caller zeroes it).  Arithmetic in float32, one rounding when a result is stored.  A row with an
- * infinity or a NaN gives unspecified values in that row alone.
+ * infinity or a NaN gives unspecified values in that row alone, and so does one whose sum of squares float32 does not hold (numbers of 2^60 and more; with
+ * eps = 0 a row without any of 2^-60 and more); backward such a row spoils the sums of dw with it.
  *
  * marl_qk_norm_rope_backward: from dq_out / dk_out, the gradients of q_out / k_out (strides q_out_stride / k_out_stride), and q, k:
  *   dy = the rotation's transpose of dz;  g_d = dy_d w_d,  n_d = x_d r,

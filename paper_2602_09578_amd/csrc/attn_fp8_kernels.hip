@@ -138,7 +138,9 @@ __device__ __forceinline__ SuffixItem suffix_item(const AttnArgs& a, int index) 
 // sums over 2^21 tokens finite for values below 2^100.
 //   Blocks of up to 256 rows (kHalves): half of the tiles each for two workgroups that run on the same XCD, as in attn_kernels.hip; their
 // keys and values are ordinary cached loads.
-//   What bounds them: the issue of instructions.  A step of a wave with two tiles is about 560 of them, 64 of these matrix instructions.  16 prefixes
+//   What bounds them: waits between two waves a SIMD.  No unit is full (of the busy time the vector ALU issues in 53 %, the matrix pipe works in 25 %, and in a
+// third nothing is issued): waves stand at waits and barriers in 38 % of their cycles and wait for their turn in 24 %.  Memory is not the cause.  A step of a wave with two tiles is about 560
+// instructions, 64 of these matrix instructions; a wave that has tiles converts all of a step's codes itself where there are five tiles or more.  16 prefixes
 // of 4096 tokens for 224 rows, 4 KV heads, 30 GFLOP: 57 us in the items kernel (0.53 PFLOP/s), the same on pages that the caches hold.  Measured
 // and left out: scores by products of 8-bit numbers (the queries as two of them each: 71 us a call instead of 74, but calls bound by memory
 // 0.5 to 1 % slower), one half of a step's weights beside the other half's scores (3 % slower), chunks of twice the default (88 us).

@@ -9,7 +9,9 @@
 //
 // What bounds it: memory.  Every head is read once and written once, so a wave keeps as many rows under way as its registers
 // hold: D / 8 lanes take a head (16 or 32 bytes a lane), a wave's step is 64 * 8 / D heads, and a wave has kSteps of them of one
-// token, whose table row it needs once.
+// token, whose table row it needs once.  65543 tokens of 28 + 4 heads of 128 in bf16, 1075 MB: 178 us (6.0 TB/s); the gradient of 32771, 806 MB: 150 us.
+// A step is of queries or of keys alone, so few small heads leave lanes without a row: 4 + 4 heads of 64 use half of them, 3.3 to 4.1 TB/s.  One list of both
+// takes these from 182 to 151 us, their gradient from 300 to 228, but costs others 0.5 to 6 % (28 + 4 of 128, 8 + 2 of 64).
 #include <algorithm>
 #include <type_traits>
 
@@ -320,12 +322,12 @@ __global__ __launch_bounds__(kFinishThreads) void qk_norm_weight_grad_kernel(Nor
   if (out) out[column < D ? column : column - D] = v;
 }
 
-// A wave's steps at once: four, where there are waves enough for the GPU's 256 CUs (eight: 189 instead of 182 us for 65543 tokens of 28
-// + 4 heads of 128, two 169 instead of 161 for the gradient of 32771); few, where a call is small and waits for its loads.
+// A wave's steps at once: four, where there are waves enough for the GPU's 256 CUs (eight: 177 instead of 180 us for 65543 tokens of 28
+// + 4 heads of 128, two 161 instead of 151 for the gradient of 32771); few, where a call is small and waits for its loads.
 constexpr int kManySteps = 4, kFewSteps = 2, kBackwardSteps = 4, kBackwardStepsF32 = 2;
 constexpr long kEnoughUnits = 8192;
-// bf16 results that the caches of the XCDs (4 MB each) cannot hold until somebody reads them are stored past them: 194 -> 187 us for the
-// 65543 tokens, 170 -> 161 for the gradient of 32771.
+// bf16 results that the caches of the XCDs (4 MB each) cannot hold until somebody reads them are stored past them: 191 -> 180 us for the
+// 65543 tokens, 162 -> 151 for the gradient of 32771.
 constexpr long kCacheBytes = 32l << 20;
 bool past_caches(const NormRopeArgs& a) { return !a.f32 && (long)a.T * (a.Hq + a.Hkv) * a.D * 2 > kCacheBytes; }
 
